@@ -378,4 +378,88 @@ struct TfEmbGradArgs {
 };
 hipError_t launch_tf_emb_grad(const TfEmbGradArgs& a, hipStream_t s);
 
+// ---------------------------------------------------------------------------
+// operators of a transformer block (ops.hip); pointers of element type fp32
+// or, with bf16 set, bf16
+// ---------------------------------------------------------------------------
+// Division of 32-bit numbers by a number fixed per launch (Granlund and
+// Montgomery 1994, "Division by invariant integers using multiplication"):
+// with l = ceil(log2 d), m = floor(2^32 (2^l - d) / d) + 1 and t = high word of
+// m n, n / d = (t + ((n - t) >> min(l, 1))) >> max(l - 1, 0) for every n.
+struct FastDiv {
+  uint32_t d, m, s1, s2;
+};
+inline FastDiv fast_div(uint32_t d) {
+  uint32_t l = 0;
+  while (l < 32 && (uint64_t(1) << l) < d) ++l;
+  return {d, uint32_t(((uint64_t(1) << 32) * ((uint64_t(1) << l) - d)) / d + 1), l < 1 ? l : 1u, l > 1 ? l - 1 : 0u};
+}
+
+// Rotary positions of q and k ([batch][seq][heads][head_dim] by strides);
+// table: rot / 2 turn fractions, then the amplitude (bits of a float in the low
+// word).  inverse: by the negative angle.  positions NULL: start + t.
+struct RopeArgs {
+  const void* x[2]; void* y[2];          // q and k
+  int64_t xs[2][3], ys[2][3];            // batch, position, head
+  int heads[2];
+  int batch, seq, dim, rot;
+  const int32_t* positions; int64_t pos_b, pos_t;
+  int64_t start, start_t;                // position start + start_t t where positions is NULL
+  const uint64_t* table;
+  int interleaved, inverse;
+};
+constexpr int kRopeFill = 128;  // table entries of one launch
+struct RopeFillArgs {
+  uint64_t* table;
+  int n;
+  uint64_t v[kRopeFill];
+};
+hipError_t launch_rope_fill(const RopeFillArgs& a, hipStream_t s);
+hipError_t launch_rope(int bf16, const RopeArgs& a, hipStream_t s);
+
+// Layer norm; w, b, mean and rstd as in the C ABI (nullable).
+struct NormArgs {
+  const void* x; int64_t ldx;
+  const float* w; const float* b;
+  void* y; int64_t ldy;
+  float* mean; float* rstd;
+  int64_t rows;
+  int cols;
+  float eps;
+};
+hipError_t launch_norm(int bf16, const NormArgs& a, hipStream_t s);
+
+// Its backward: dx (nullable) and, over norm_bwd_parts() slices of the rows,
+// partial sums part[slice][0: dw, 1: db][ldpart] (part nullable), which
+// launch_norm_sum adds in order into dw and db (each nullable).
+struct NormBwdArgs {
+  const void* x; int64_t ldx;
+  const void* dy; int64_t lddy;
+  const float* w; const float* mean; const float* rstd;
+  const void* res; int64_t ldres;
+  void* dx; int64_t lddx;
+  float* part; int64_t ldpart; int nparts;
+  int64_t rows;
+  int cols;
+};
+int norm_bwd_parts(int bf16, int64_t rows, int cols);
+inline int64_t norm_part_pitch(int cols) { return (cols + 3) / 4 * 4; }
+hipError_t launch_norm_bwd(int bf16, const NormBwdArgs& a, hipStream_t s);
+hipError_t launch_norm_sum(const float* part, int64_t ldpart, int nparts, int cols, float* dw, float* db, hipStream_t s);
+
+// Dropout (+ residual, nullable): element (row0 + r, c) is kept where its 16
+// random bits are at least `limit`, and scaled.
+struct DropArgs {
+  const void* x; int64_t ldx;
+  const void* res; int64_t ldres;
+  void* y; int64_t ldy;
+  int64_t rows, row0;
+  int cols;
+  uint64_t seed, offset;
+  const uint64_t* step;  // nullable: added to offset
+  uint32_t limit;
+  float scale;
+};
+hipError_t launch_dropout(int bf16, const DropArgs& a, hipStream_t s);
+
 }  // namespace erase

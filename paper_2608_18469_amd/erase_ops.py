@@ -1,0 +1,368 @@
+"""Python binding of the transformer operators of liberase.so (the C ABI in
+include/erase_ops.h): rotary positions, layer norm and dropout, each with its
+backward pass, on device tensors.
+
+Argument marshalling only: every operator runs in the HIP kernels behind the C
+ABI; PyTorch provides device memory and streams.  There is no fallback and no
+autograd: the backward passes are calls of their own.  Each function enqueues
+on ``stream`` (a torch stream of the tensors' device; default: that device's
+current stream), returns without waiting, and allocates the outputs that
+``out`` does not give.
+"""
+from __future__ import annotations
+
+import ctypes
+from ctypes import POINTER, c_double, c_float, c_int32, c_int64, c_size_t, c_uint64, c_void_p
+
+from . import erase
+from .erase import BF16, ERR_INVALID_ARG, ERR_SHAPE, ERR_WORKSPACE, F32, OK, EraseError
+
+LAYOUTS = {"half": 0, "interleaved": 1}
+SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "by_parts": 3}
+
+
+class RopeSpec(ctypes.Structure):
+    """erase_rope_spec: which frequencies a table holds."""
+    _fields_ = [("rot_dim", c_int32), ("scaling", c_int32), ("base", c_double), ("factor", c_double),
+                ("original_length", c_double), ("fast", c_double), ("slow", c_double)]
+
+
+class RopeConfig(ctypes.Structure):
+    """erase_rope_config: shape of one rotation."""
+    _fields_ = [("dtype", c_int32), ("layout", c_int32), ("batch", c_int32), ("seq", c_int32), ("q_heads", c_int32),
+                ("k_heads", c_int32), ("head_dim", c_int32), ("rot_dim", c_int32), ("q_stride", c_int64 * 3),
+                ("k_stride", c_int64 * 3), ("qo_stride", c_int64 * 3), ("ko_stride", c_int64 * 3),
+                ("pos_stride", c_int64), ("start", c_int64)]
+
+
+class NormConfig(ctypes.Structure):
+    """erase_norm_config: shape of a layer norm and its backward pass."""
+    _fields_ = [("rows", c_int64), ("cols", c_int32), ("dtype", c_int32), ("eps", c_float), ("x_ld", c_int64),
+                ("y_ld", c_int64), ("dy_ld", c_int64), ("dx_ld", c_int64), ("res_ld", c_int64)]
+
+
+class DropoutConfig(ctypes.Structure):
+    """erase_dropout_config: shape, probability and place in the random stream."""
+    _fields_ = [("rows", c_int64), ("cols", c_int64), ("dtype", c_int32), ("p", c_double), ("seed", c_uint64),
+                ("offset", c_uint64), ("x_ld", c_int64), ("res_ld", c_int64), ("y_ld", c_int64)]
+
+
+# every entry point of include/erase_ops.h with its ctypes signature
+SIGNATURES = {
+    "erase_rope_frequencies": (c_int32, [POINTER(RopeSpec), POINTER(c_double), POINTER(c_double)]),
+    "erase_rope_table_bytes": (c_int32, [POINTER(RopeSpec), POINTER(c_size_t)]),
+    "erase_rope_table": (c_int32, [POINTER(RopeSpec), c_void_p, c_void_p]),
+    "erase_rope": (c_int32, [POINTER(RopeConfig)] + [c_void_p] * 7),
+    "erase_rope_backward": (c_int32, [POINTER(RopeConfig)] + [c_void_p] * 7),
+    "erase_layer_norm": (c_int32, [POINTER(NormConfig)] + [c_void_p] * 7),
+    "erase_layer_norm_backward_scratch_bytes": (c_int32, [POINTER(NormConfig), POINTER(c_size_t)]),
+    "erase_layer_norm_backward": (c_int32, [POINTER(NormConfig)] + [c_void_p] * 10 + [c_size_t, c_void_p]),
+    "erase_dropout": (c_int32, [POINTER(DropoutConfig)] + [c_void_p] * 5),
+    "erase_dropout_backward": (c_int32, [POINTER(DropoutConfig)] + [c_void_p] * 4),
+}
+
+_lib = None
+
+
+def lib() -> ctypes.CDLL:
+    global _lib
+    if _lib is None:
+        L = erase.lib()
+        for name, (res, args) in SIGNATURES.items():
+            f = getattr(L, name)
+            f.restype = res
+            f.argtypes = args
+        _lib = L
+    return _lib
+
+
+def _check(status: int, where: str):
+    if status != OK:
+        raise EraseError(status, where)
+
+
+def _dtype(where: str, name: str, t) -> int:
+    import torch
+    if t.dtype == torch.bfloat16:
+        return BF16
+    if t.dtype == torch.float32:
+        return F32
+    raise EraseError(ERR_INVALID_ARG, where, f"{name} must be float32 or bfloat16")
+
+
+def _on(where: str, x, **others):
+    """Every tensor on x's GPU."""
+    if not x.is_cuda:
+        raise EraseError(ERR_INVALID_ARG, where, "tensors must be on the GPU")
+    dev = x.get_device()
+    for name, t in others.items():
+        if t is not None and t.get_device() != dev:
+            raise EraseError(ERR_INVALID_ARG, where, f"{name} is not on the GPU of the other tensors")
+    return dev
+
+
+def _like(where: str, name: str, t, x):
+    if t.dtype != x.dtype or t.shape != x.shape:
+        raise EraseError(ERR_SHAPE if t.dtype == x.dtype else ERR_INVALID_ARG, where,
+                         f"{name} must have the type {x.dtype} and the shape {list(x.shape)}")
+
+
+def _vector(where: str, name: str, t, n: int):
+    import torch
+    if t is not None and (t.dtype != torch.float32 or t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1)):
+        raise EraseError(ERR_INVALID_ARG, where, f"{name} must be a contiguous float32 tensor of {n}")
+
+
+def _run(where: str, fn, dev: int, stream, *args):
+    """fn(*args, stream handle) with dev as the current device."""
+    import torch
+    if stream is not None and stream.device.index != dev:
+        raise EraseError(ERR_INVALID_ARG, where, "stream is not one of the tensors' GPU")
+    if dev == torch.cuda.current_device():
+        _check(fn(*args, (stream or torch.cuda.current_stream(dev)).cuda_stream), where)
+        return
+    with torch.cuda.device(dev):
+        _check(fn(*args, (stream or torch.cuda.current_stream(dev)).cuda_stream), where)
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+# ---------------------------------------------------------------------------
+# rotary positions
+# ---------------------------------------------------------------------------
+def _rope_spec(rot_dim, base, scaling, factor, original_length, fast, slow) -> RopeSpec:
+    if scaling not in SCALINGS:
+        raise EraseError(ERR_INVALID_ARG, "rope", f"scaling must be one of {sorted(SCALINGS)}")
+    return RopeSpec(rot_dim, SCALINGS[scaling], base, factor, original_length, fast, slow)
+
+
+def rope_frequencies(rot_dim, base=10000.0, scaling="none", factor=1.0, original_length=0.0, fast=32.0, slow=1.0):
+    """(angles per position of the rot_dim / 2 pairs, amplitude) on the host (erase_rope_frequencies)."""
+    spec = _rope_spec(rot_dim, base, scaling, factor, original_length, fast, slow)
+    freq, amp = (c_double * max(1, rot_dim // 2))(), c_double(0)
+    _check(lib().erase_rope_frequencies(ctypes.byref(spec), freq, ctypes.byref(amp)), "erase_rope_frequencies")
+    return list(freq), amp.value
+
+
+class RopeTable:
+    """A device table of erase_rope_table: read only, for any number of calls."""
+
+    def __init__(self, spec: RopeSpec, data):
+        self.rot_dim, self.data = spec.rot_dim, data
+
+
+def rope_table(rot_dim, base=10000.0, scaling="none", factor=1.0, original_length=0.0, fast=32.0, slow=1.0, device=None,
+               stream=None) -> RopeTable:
+    """The table of a rotation (erase_rope_spec's fields) on `device` (default: the
+    current GPU), filled on `stream`; calls on another stream wait for it."""
+    import torch
+    spec = _rope_spec(rot_dim, base, scaling, factor, original_length, fast, slow)
+    n = c_size_t(0)
+    _check(lib().erase_rope_table_bytes(ctypes.byref(spec), ctypes.byref(n)), "erase_rope_table_bytes")
+    if not torch.cuda.is_available():
+        raise RuntimeError("no HIP device available: the operators run only on the GPU")
+    dev = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
+    data = torch.empty(n.value // 8, dtype=torch.int64, device=dev)
+    _run("erase_rope_table", lib().erase_rope_table, data.get_device(), stream, ctypes.byref(spec), data.data_ptr())
+    return RopeTable(spec, data)
+
+
+def _rotate(where, fn, q, k, table, positions, start, layout, out, stream):
+    import torch
+    if layout not in LAYOUTS:
+        raise EraseError(ERR_INVALID_ARG, where, f"layout must be one of {sorted(LAYOUTS)}")
+    for name, t in (("q", q), ("k", k)):
+        if t is not None and (t.dim() != 4 or (t.shape[3] > 1 and t.stride(3) != 1)):
+            raise EraseError(ERR_SHAPE, where, f"{name} must be [batch][seq][heads][head_dim] with contiguous columns")
+    B, T, Hq, D = q.shape
+    dt = _dtype(where, "q", q)
+    if k is not None and (k.dtype != q.dtype or k.shape[:2] != q.shape[:2] or k.shape[3] != D):
+        raise EraseError(ERR_SHAPE, where, "k must have q's type, batch, length and head size")
+    dev = _on(where, q, k=k, table=table.data, positions=positions)
+    pos_stride = 0
+    if positions is not None:
+        if positions.dtype != torch.int32 or positions.shape != q.shape[:2] or (T > 1 and positions.stride(1) != 1):
+            raise EraseError(ERR_INVALID_ARG, where, "positions must be int32 [batch][seq] with unit stride along seq")
+        pos_stride = positions.stride(0)
+    if out is None:
+        qo = torch.empty((B, T, Hq, D), dtype=q.dtype, device=q.device)
+        ko = None if k is None else torch.empty(k.shape, dtype=k.dtype, device=k.device)
+    else:
+        qo, ko = out
+        for name, o, t in (("out[0]", qo, q), ("out[1]", ko, k)):
+            if (o is None) != (t is None):
+                raise EraseError(ERR_INVALID_ARG, where, f"{name} must be given exactly where its input is")
+            if o is not None:
+                _like(where, name, o, t)
+                if D > 1 and o.stride(3) != 1:
+                    raise EraseError(ERR_SHAPE, where, f"{name} must have contiguous columns")
+        _on(where, q, out0=qo, out1=ko)
+    zero = (0, 0, 0, 0)
+    kh, ks, kos = (0, zero, zero) if k is None else (k.shape[2], k.stride(), ko.stride())
+    three = c_int64 * 3
+    cfg = RopeConfig(dt, LAYOUTS[layout], B, T, Hq, kh, D, table.rot_dim, three(*q.stride()[:3]), three(*ks[:3]),
+                     three(*qo.stride()[:3]), three(*kos[:3]), pos_stride, start)
+    _run(where, fn, dev, stream, ctypes.byref(cfg), q.data_ptr(), _ptr(k), qo.data_ptr(), _ptr(ko), _ptr(positions),
+         table.data.data_ptr())
+    return qo, ko
+
+
+def rope(q, k, table, positions=None, start=0, layout="half", out=None, stream=None):
+    """Queries q [batch][seq][heads][head_dim] and keys k (fewer heads, or None)
+    rotated by their positions (erase_rope): position start + t, or `positions`
+    int32 [batch][seq].  `table` is rope_table()'s; its rot_dim columns of every
+    head turn, pairs (i, i + rot_dim / 2) with layout "half" and (2 i, 2 i + 1)
+    with "interleaved".  Strides are free but for contiguous columns; ``out`` may
+    be (q, k) themselves.  Returns (q_out, k_out)."""
+    return _rotate("erase_rope", lib().erase_rope, q, k, table, positions, start, layout, out, stream)
+
+
+def rope_backward(dq, dk, table, positions=None, start=0, layout="half", out=None, stream=None):
+    """Gradients at q and k from those at rope()'s outputs (erase_rope_backward);
+    arguments as for rope()."""
+    return _rotate("erase_rope_backward", lib().erase_rope_backward, dq, dk, table, positions, start, layout, out, stream)
+
+
+# ---------------------------------------------------------------------------
+# layer norm
+# ---------------------------------------------------------------------------
+def _matrix(where: str, name: str, t):
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise EraseError(ERR_SHAPE, where, f"{name} must be [rows][cols] with unit column stride")
+
+
+def layer_norm(x, weight=None, bias=None, eps=1e-5, out=None, stream=None):
+    """Layer norm of the rows of x [rows][cols] (erase_layer_norm), weight and
+    bias float32 [cols] or None.  Returns (y, mean, rstd), the float32 statistics
+    [rows] for the backward pass.  ``out`` gives the three; its statistics may be
+    None (not computed), its y may be x."""
+    import torch
+    where = "erase_layer_norm"
+    _matrix(where, "x", x)
+    dt = _dtype(where, "x", x)
+    R, C = x.shape
+    _vector(where, "weight", weight, C)
+    _vector(where, "bias", bias, C)
+    dev = _on(where, x, weight=weight, bias=bias)
+    if out is None:
+        y = torch.empty((R, C), dtype=x.dtype, device=x.device)
+        mean, rstd = (torch.empty(R, dtype=torch.float32, device=x.device) for _ in range(2))
+    else:
+        y, mean, rstd = out
+        _like(where, "out[0]", y, x)
+        _matrix(where, "out[0]", y)
+        _vector(where, "out[1]", mean, R)
+        _vector(where, "out[2]", rstd, R)
+        _on(where, x, out0=y, out1=mean, out2=rstd)
+    cfg = NormConfig(R, C, dt, eps, x.stride(0), y.stride(0), 0, 0, 0)
+    _run(where, lib().erase_layer_norm, dev, stream, ctypes.byref(cfg), x.data_ptr(), _ptr(weight), _ptr(bias),
+         y.data_ptr(), _ptr(mean), _ptr(rstd))
+    return y, mean, rstd
+
+
+def _norm_scratch_bytes(cfg: NormConfig) -> int:
+    n = c_size_t(0)
+    _check(lib().erase_layer_norm_backward_scratch_bytes(ctypes.byref(cfg), ctypes.byref(n)),
+           "erase_layer_norm_backward_scratch_bytes")
+    return n.value
+
+
+def layer_norm_backward_scratch(x):
+    """Scratch of layer_norm_backward() for tensors of x's shape and type; one for
+    every call in flight."""
+    import torch
+    where = "erase_layer_norm_backward"
+    _matrix(where, "x", x)
+    cfg = NormConfig(x.shape[0], x.shape[1], _dtype(where, "x", x), 0.0, 0, 0, 0, 0, 0)
+    return torch.empty(_norm_scratch_bytes(cfg), dtype=torch.uint8, device=x.device)
+
+
+def layer_norm_backward(dy, x, weight, mean, rstd, residual=None, need_input=True, need_weight=True, need_bias=True,
+                        out=None, scratch=None, stream=None):
+    """Gradients (dx, dweight, dbias) of layer_norm() (erase_layer_norm_backward)
+    from dy and the forward's x, weight, mean and rstd; `residual` (a gradient of
+    x's shape, or None) is added to dx.  What is not needed is returned as None.
+    ``out`` gives the three (dx may be dy or residual), ``scratch``
+    layer_norm_backward_scratch()'s memory (allocated unless given)."""
+    import torch
+    where = "erase_layer_norm_backward"
+    _matrix(where, "x", x)
+    dt = _dtype(where, "x", x)
+    R, C = x.shape
+    _like(where, "dy", dy, x)
+    _matrix(where, "dy", dy)
+    _vector(where, "weight", weight, C)
+    _vector(where, "mean", mean, R)
+    _vector(where, "rstd", rstd, R)
+    if residual is not None:
+        _like(where, "residual", residual, x)
+        _matrix(where, "residual", residual)
+    dev = _on(where, x, dy=dy, weight=weight, mean=mean, rstd=rstd, residual=residual, scratch=scratch)
+    dx = dw = db = None
+    if out is not None:
+        dx, dw, db = out
+        if dx is not None:
+            _like(where, "out[0]", dx, x)
+            _matrix(where, "out[0]", dx)
+        _vector(where, "out[1]", dw, C)
+        _vector(where, "out[2]", db, C)
+        _on(where, x, out0=dx, out1=dw, out2=db)
+    dx = (dx if dx is not None else torch.empty((R, C), dtype=x.dtype, device=x.device)) if need_input else None
+    dw = (dw if dw is not None else torch.empty(C, dtype=torch.float32, device=x.device)) if need_weight else None
+    db = (db if db is not None else torch.empty(C, dtype=torch.float32, device=x.device)) if need_bias else None
+    cfg = NormConfig(R, C, dt, 0.0, x.stride(0), 0, dy.stride(0), 0 if dx is None else dx.stride(0),
+                     0 if residual is None else residual.stride(0))
+    if scratch is not None and not scratch.is_contiguous():
+        raise EraseError(ERR_WORKSPACE, where, "scratch must be contiguous")
+    if scratch is None and (need_weight or need_bias):
+        scratch = torch.empty(_norm_scratch_bytes(cfg), dtype=torch.uint8, device=x.device)
+    _run(where, lib().erase_layer_norm_backward, dev, stream, ctypes.byref(cfg), x.data_ptr(), dy.data_ptr(), _ptr(weight),
+         _ptr(mean), _ptr(rstd), _ptr(residual), _ptr(dx), _ptr(dw), _ptr(db), _ptr(scratch),
+         0 if scratch is None else scratch.numel() * scratch.element_size())
+    return dx, dw, db
+
+
+# ---------------------------------------------------------------------------
+# dropout
+# ---------------------------------------------------------------------------
+def _drop(where, fn, x, p, seed, offset, residual, step, out, stream):
+    import torch
+    _matrix(where, "x", x)
+    dt = _dtype(where, "x", x)
+    if not 0 <= seed < 1 << 64 or not 0 <= offset < 1 << 64:
+        raise EraseError(ERR_INVALID_ARG, where, "seed and offset must be 64-bit unsigned numbers")
+    if residual is not None:
+        _like(where, "residual", residual, x)
+        _matrix(where, "residual", residual)
+    if step is not None and (step.dtype not in (torch.int64, torch.uint64) or step.numel() != 1):
+        raise EraseError(ERR_INVALID_ARG, where, "step must be one int64 or uint64 on the device")
+    dev = _on(where, x, residual=residual, step=step, out=out)
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    else:
+        _like(where, "out", out, x)
+        _matrix(where, "out", out)
+    cfg = DropoutConfig(x.shape[0], x.shape[1], dt, p, seed, offset, x.stride(0),
+                        0 if residual is None else residual.stride(0), out.stride(0))
+    if fn == "erase_dropout":
+        args = (x.data_ptr(), _ptr(residual), out.data_ptr(), _ptr(step))
+    else:
+        args = (x.data_ptr(), out.data_ptr(), _ptr(step))
+    _run(where, getattr(lib(), fn), dev, stream, ctypes.byref(cfg), *args)
+    return out
+
+
+def dropout(x, p, seed, offset=0, residual=None, step=None, out=None, stream=None):
+    """residual + dropout of x [rows][cols] with probability p (erase_dropout):
+    the mask is a function of (seed, offset + step, row, column).  `step` is an
+    int64 or uint64 [1] on the device (or None), read when the launch runs.
+    ``out`` may be x or residual.  Returns y."""
+    return _drop("erase_dropout", "erase_dropout", x, p, seed, offset, residual, step, out, stream)
+
+
+def dropout_backward(dy, p, seed, offset=0, step=None, out=None, stream=None):
+    """The gradient at dropout()'s x from that at its output, for the same p, seed,
+    offset and step (erase_dropout_backward).  ``out`` may be dy."""
+    return _drop("erase_dropout_backward", "erase_dropout_backward", dy, p, seed, offset, None, step, out, stream)
