@@ -7,6 +7,7 @@
 
 #include <algorithm>
 #include <cstdint>
+#include <type_traits>
 
 #include "device.h"
 #include "internal.h"
@@ -21,6 +22,82 @@ hipError_t launch1(void (*kernel)(A), int64_t grid, int block, const A& a, hipSt
   A copy = a;
   void* args[] = {&copy};
   return hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3((uint32_t)grid), dim3((uint32_t)block), args, 0, s);
+}
+
+// Eight bf16 or four fp32 consecutive elements, moved by one 16-byte access from
+// any element's address (the hardware splits what straddles a line), or one by
+// one where fewer than that are left.  Elements past the end are zero.
+typedef uint32_t u32x4_at2_t __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t u32x4_at4_t __attribute__((ext_vector_type(4), aligned(4)));
+template <typename T>
+struct Chunk {
+  static constexpr int V = 16 / sizeof(T);
+  typedef std::conditional_t<sizeof(T) == 2, u32x4_at2_t, u32x4_at4_t> mem_t;
+  u32x4_t r;
+  __device__ __forceinline__ float operator[](int k) const {
+    if constexpr (sizeof(T) == 4)
+      return __uint_as_float(r[k]);
+    else
+      return __uint_as_float(k & 1 ? r[k >> 1] & 0xffff0000u : r[k >> 1] << 16);
+  }
+};
+template <typename T>
+__device__ __forceinline__ Chunk<T> ld_chunk(const T* p, int n) {
+  Chunk<T> c;
+  if (n >= Chunk<T>::V) {
+    c.r = *reinterpret_cast<const typename Chunk<T>::mem_t*>(p);
+  } else {
+    c.r = u32x4_t{0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int k = 0; k < Chunk<T>::V - 1; ++k)
+      if (k < n) {
+        if constexpr (sizeof(T) == 4)
+          c.r[k] = __float_as_uint(p[k]);
+        else
+          c.r[k >> 1] |= (uint32_t)p[k] << (16 * (k & 1));
+      }
+  }
+  return c;
+}
+template <typename T>
+__device__ __forceinline__ void st_chunk(T* p, int n, const float v[Chunk<T>::V]) {
+  if (n >= Chunk<T>::V) {
+    u32x4_t r;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if constexpr (sizeof(T) == 4)
+        r[k] = __float_as_uint(v[k]);
+      else
+        r[k] = (uint32_t)f2bf(v[2 * k]) | ((uint32_t)f2bf(v[2 * k + 1]) << 16);
+    }
+    *reinterpret_cast<typename Chunk<T>::mem_t*>(p) = r;
+  } else {
+#pragma unroll
+    for (int k = 0; k < Chunk<T>::V - 1; ++k)
+      if (k < n) p[k] = cvt<T>(v[k]);
+  }
+}
+
+// Sum over groups of L = 16 or 64 lanes, the same bits in every lane: within 16
+// lanes by lane permutations in the add itself (xor 1, xor 2, mirrored halves,
+// mirrored rows), beyond by exchanging rows and halves.
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) {
+  return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), CTRL, 0xf, 0xf, true));
+}
+template <int L>
+__device__ __forceinline__ float lane_sum(float v) {
+  v += dpp<0xb1>(v);
+  v += dpp<0x4e>(v);
+  v += dpp<0x141>(v);
+  v += dpp<0x140>(v);
+  if constexpr (L == 64) {
+    auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(b[0]) + __uint_as_float(b[1]);
+  }
+  return v;
 }
 
 // sine and cosine of a 64-bit fraction of a turn: the quadrant from the top
@@ -146,46 +223,184 @@ hipError_t launch_norm(int bf16, const NormArgs& a, hipStream_t s) {
   return launch1(bf16 ? ops_norm<uint16_t> : ops_norm<float>, std::min<int64_t>(a.rows, 1 << 20), 256, a, s);
 }
 
-// Workgroup g takes rows g, g + nparts, ...; its weight gradients pass through
-// its slice of `part`, every column by one thread.
-template <typename T>
-__global__ __launch_bounds__(256) void ops_norm_bwd(NormBwdArgs a) {
-  float* pw = a.part ? a.part + (int64_t)blockIdx.x * 2 * a.ldpart : nullptr;
-  float* pb = a.part ? pw + a.ldpart : nullptr;
-  if (pw)
-    for (int c = threadIdx.x; c < a.cols; c += 256) pw[c] = pb[c] = 0.f;
-  for (int64_t n = blockIdx.x; n < a.rows; n += gridDim.x) {
-    const T* x = static_cast<const T*>(a.x) + n * a.ldx;
-    const T* dy = static_cast<const T*>(a.dy) + n * a.lddy;
-    const T* res = a.res ? static_cast<const T*>(a.res) + n * a.ldres : nullptr;
-    T* dx = a.dx ? static_cast<T*>(a.dx) + n * a.lddx : nullptr;
-    const float mean = a.mean[n], r = a.rstd[n];
-    float sg = 0.f, sgh = 0.f;
-    for (int c = threadIdx.x; c < a.cols; c += 256) {
-      const float d = ldf(dy + c), h = (ldf(x + c) - mean) * r, g = d * (a.w ? a.w[c] : 1.f);
-      sg += g;
-      sgh = fmaf(g, h, sgh);
-      if (pw) {
-        pw[c] = fmaf(d, h, pw[c]);
-        pb[c] += d;
-      }
+// Layouts of the row kernels: a row is held by `lanes` threads (16 of a wave, a
+// wave, or W waves), K chunks of 16 bytes each, `groups` rows at a time in a
+// workgroup of 256 or 512 threads.
+template <typename E, int Lanes, int Waves, int Chunks>
+struct RowShape {
+  typedef E T;
+  static constexpr int L = Lanes, W = Waves, K = Chunks;
+  static constexpr int lanes = L * W, groups = L == 16 ? 16 : W == 1 ? 4 : W == 4 ? 2 : 1;
+  static constexpr int threads = lanes * groups, cols = lanes * K * Chunk<T>::V;
+  static constexpr bool ahead = cols / lanes < 32;  // the backward holds the next row as well (registers)
+};
+
+namespace {
+
+// A thread's part of x and dy of row n, and the row's statistics; zeros behind
+// the last row, which add nothing.
+template <typename S>
+struct NormRow {
+  Chunk<typename S::T> x[S::K], d[S::K];
+  float mean, r;
+};
+template <typename S>
+__device__ __forceinline__ NormRow<S> ld_norm_row(const NormBwdArgs& a, int64_t n, int pos) {
+  typedef typename S::T T;
+  NormRow<S> v;
+  const bool row = n < a.rows;
+  v.mean = row ? a.mean[n] : 0.f;
+  v.r = row ? a.rstd[n] : 0.f;
+#pragma unroll
+  for (int i = 0; i < S::K; ++i) {
+    const int c = (pos + i * S::lanes) * Chunk<T>::V;
+    const int left = row ? a.cols - c : 0;
+    v.x[i] = ld_chunk(static_cast<const T*>(a.x) + n * a.ldx + c, left);
+    v.d[i] = ld_chunk(static_cast<const T*>(a.dy) + n * a.lddy + c, left);
+  }
+  return v;
+}
+
+// A workgroup's sums of its rows' columns: row groups added in order in LDS.
+template <typename S, typename A>
+__device__ __forceinline__ void st_norm_part(const A& acc, float* comb, int grp, int pos, int cols, float* part) {
+  constexpr int V = Chunk<typename S::T>::V;
+#pragma unroll
+  for (int i = 0; i < S::K; ++i)
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+      const int c = (pos + i * S::lanes) * V + k;
+      if constexpr (S::groups > 1)
+        comb[grp * S::cols + c] = acc[i][k];
+      else if (c < cols)
+        part[c] = acc[i][k];
     }
-    block_sum2(sg, sgh);
-    if (!dx) continue;
-    const float mg = sg / (float)a.cols, mgh = sgh / (float)a.cols;
-    for (int c = threadIdx.x; c < a.cols; c += 256) {
-      const float h = (ldf(x + c) - mean) * r, g = ldf(dy + c) * (a.w ? a.w[c] : 1.f);
-      dx[c] = cvt<T>(fmaf(r, g - mg - h * mgh, res ? ldf(res + c) : 0.f));
+  if constexpr (S::groups > 1) {
+    __syncthreads();
+    for (int c = threadIdx.x; c < cols; c += S::threads) {
+      float v = comb[c];
+#pragma unroll
+      for (int g = 1; g < S::groups; ++g) v += comb[g * S::cols + c];
+      part[c] = v;
     }
   }
 }
 
-int norm_bwd_parts(int, int64_t rows, int) { return (int)std::max<int64_t>(1, std::min<int64_t>(rows, 1024)); }
+}  // namespace
 
-hipError_t launch_norm_bwd(int bf16, const NormBwdArgs& a, hipStream_t s) {
-  return launch1(bf16 ? ops_norm_bwd<uint16_t> : ops_norm_bwd<float>, a.nparts, 256, a, s);
+// Backward.  A thread keeps its columns' weights and its partial sums of dw and
+// db in registers over all its rows; the loads of the next row are in flight
+// while the current one is reduced.  At the end the workgroup's row groups are
+// added in order through LDS, and one partial row per workgroup is stored.
+template <typename S>
+__global__ __launch_bounds__(S::threads) void ops_norm_bwd(NormBwdArgs a) {
+  typedef typename S::T T;
+  constexpr int V = Chunk<T>::V, G = S::groups, L = S::L, W = S::W, K = S::K;
+  __shared__ float2 sums[2][G][W];
+  __shared__ float comb[G > 1 ? G * S::cols : 1];
+  const int grp = threadIdx.x / S::lanes, pos = threadIdx.x % S::lanes;
+  float w[K][V], aw[K][V], ab[K][V];
+#pragma unroll
+  for (int i = 0; i < K; ++i) {
+    const int c = (pos + i * S::lanes) * V;
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+      w[i][k] = a.w && c + k < a.cols ? a.w[c + k] : 1.f;
+      aw[i][k] = ab[i][k] = 0.f;
+    }
+  }
+  const float inv = 1.f / (float)a.cols;
+  const int64_t step = (int64_t)gridDim.x * G;
+  int64_t n = (int64_t)blockIdx.x * G + grp;
+  NormRow<S> next;
+  if constexpr (S::ahead) next = ld_norm_row<S>(a, n, pos);
+  int buf = 0;
+  // the same number of rounds for every row group of the workgroup
+  for (int64_t n0 = (int64_t)blockIdx.x * G; n0 < a.rows; n0 += step, n += step) {
+    const NormRow<S> cur = S::ahead ? next : ld_norm_row<S>(a, n, pos);
+    if constexpr (S::ahead) next = ld_norm_row<S>(a, n + step, pos);
+    float sg = 0.f, sgh = 0.f;
+#pragma unroll
+    for (int i = 0; i < K; ++i)
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        const float dv = cur.d[i][k], h = (cur.x[i][k] - cur.mean) * cur.r, g = dv * w[i][k];
+        sg += g;
+        sgh = fmaf(g, h, sgh);
+        aw[i][k] = fmaf(dv, h, aw[i][k]);
+        ab[i][k] += dv;
+      }
+    if (!a.dx) continue;
+    sg = lane_sum<L>(sg);
+    sgh = lane_sum<L>(sgh);
+    if constexpr (W > 1) {
+      if ((threadIdx.x & 63) == 0) sums[buf][grp][pos >> 6] = make_float2(sg, sgh);
+      __syncthreads();
+      sg = sgh = 0.f;
+#pragma unroll
+      for (int j = 0; j < W; ++j) {
+        sg += sums[buf][grp][j].x;
+        sgh += sums[buf][grp][j].y;
+      }
+      buf ^= 1;  // one barrier a round: the round after next writes this buffer again
+    }
+    if (n >= a.rows) continue;
+    const float mg = sg * inv, mgh = sgh * inv;
+#pragma unroll
+    for (int i = 0; i < K; ++i) {
+      const int c = (pos + i * S::lanes) * V;
+      if (c >= a.cols) continue;
+      Chunk<T> res;
+      res.r = u32x4_t{0u, 0u, 0u, 0u};
+      if (a.res) res = ld_chunk(static_cast<const T*>(a.res) + n * a.ldres + c, a.cols - c);
+      float o[V];
+#pragma unroll
+      for (int k = 0; k < V; ++k)
+        o[k] = fmaf(cur.r, cur.d[i][k] * w[i][k] - mg - (cur.x[i][k] - cur.mean) * cur.r * mgh, res[k]);
+      st_chunk(static_cast<T*>(a.dx) + n * a.lddx + c, a.cols - c, o);
+    }
+  }
+  if (!a.part) return;
+  float* part = a.part + (int64_t)blockIdx.x * 2 * a.ldpart;
+  st_norm_part<S>(aw, comb, grp, pos, a.cols, part);
+  if constexpr (G > 1) __syncthreads();
+  st_norm_part<S>(ab, comb, grp, pos, a.cols, part + a.ldpart);
 }
 
+namespace {
+
+// Calls f with the shape that holds a row of `cols` elements: 16 lanes for the
+// narrowest rows, then a wave with 1 or 2 chunks a lane, then 4 waves, then 8.
+template <typename T, typename F>
+auto with_row_shape(int cols, F&& f) {
+  constexpr int V = Chunk<T>::V;
+  if (cols <= 16 * V) return f(RowShape<T, 16, 1, 1>());
+  if (cols <= 64 * V) return f(RowShape<T, 64, 1, 1>());
+  if (cols <= 128 * V) return f(RowShape<T, 64, 1, 2>());
+  if (cols <= 256 * V) return f(RowShape<T, 64, 4, 1>());
+  if (cols <= 512 * V) return f(RowShape<T, 64, 4, 2>());
+  if (cols <= 1024 * V) return f(RowShape<T, 64, 8, 2>());
+  if constexpr (V == 4)
+    if (cols > 2048 * V) return f(RowShape<T, 64, 8, 8>());
+  return f(RowShape<T, 64, 8, 4>());
+}
+
+}  // namespace
+
+// Partial rows: one per workgroup, as many workgroups as the chip holds at
+// once at two per compute unit.
+int norm_bwd_parts(int bf16, int64_t rows, int cols) {
+  auto parts = [&](auto sh) { return (int)std::max<int64_t>(1, std::min<int64_t>((rows + sh.groups - 1) / sh.groups, 512)); };
+  return bf16 ? with_row_shape<uint16_t>(cols, parts) : with_row_shape<float>(cols, parts);
+}
+
+hipError_t launch_norm_bwd(int bf16, const NormBwdArgs& a, hipStream_t s) {
+  auto run = [&](auto sh) { return launch1(ops_norm_bwd<decltype(sh)>, a.nparts, sh.threads, a, s); };
+  return bf16 ? with_row_shape<uint16_t>(a.cols, run) : with_row_shape<float>(a.cols, run);
+}
+
+// dw and db from the partial rows ([slice][dw | db][ldpart]): 16 columns a
+// workgroup, 64 threads down the slices for each 4 of them, then a tree in LDS.
 struct NormSumArgs {
   const float* part;
   int64_t ldpart;
@@ -193,21 +408,38 @@ struct NormSumArgs {
   float *dw, *db;
 };
 __global__ __launch_bounds__(256) void ops_norm_sum(NormSumArgs a) {
-  const int c = blockIdx.x * 256 + threadIdx.x;
-  if (c >= a.cols) return;
-  float w = 0.f, b = 0.f;
-  for (int g = 0; g < a.nparts; ++g) {
-    const float* p = a.part + (int64_t)g * 2 * a.ldpart + c;
-    w += p[0];
-    b += p[a.ldpart];
+  __shared__ float4 sum[64][4];
+  const int64_t c = (int64_t)blockIdx.x * 16 + (threadIdx.x & 3) * 4;  // of dw | db, a multiple of 4
+  const int slice = threadIdx.x >> 2;
+  float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (c < 2 * a.ldpart)
+    for (int g = slice; g < a.nparts; g += 64) {
+      const float4 p = *reinterpret_cast<const float4*>(a.part + (int64_t)g * 2 * a.ldpart + c);
+      v.x += p.x, v.y += p.y, v.z += p.z, v.w += p.w;
+    }
+  sum[slice][threadIdx.x & 3] = v;
+#pragma unroll
+  for (int n = 32; n >= 1; n >>= 1) {
+    __syncthreads();
+    if (slice < n) {
+      const float4 p = sum[slice + n][threadIdx.x & 3];
+      v.x += p.x, v.y += p.y, v.z += p.z, v.w += p.w;
+      sum[slice][threadIdx.x & 3] = v;
+    }
   }
-  if (a.dw) a.dw[c] = w;
-  if (a.db) a.db[c] = b;
+  if (slice || c >= 2 * a.ldpart) return;
+  float* out = c < a.ldpart ? a.dw : a.db;
+  if (!out) return;
+  const int c0 = (int)(c < a.ldpart ? c : c - a.ldpart);
+  const float o[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    if (c0 + k < a.cols) out[c0 + k] = o[k];
 }
 
 hipError_t launch_norm_sum(const float* part, int64_t ldpart, int nparts, int cols, float* dw, float* db, hipStream_t s) {
   const NormSumArgs a{part, ldpart, nparts, cols, dw, db};
-  return launch1(ops_norm_sum, (cols + 255) / 256, 256, a, s);
+  return launch1(ops_norm_sum, (2 * ldpart + 15) / 16, 256, a, s);
 }
 
 // ---------------------------------------------------------------------------
