@@ -397,14 +397,14 @@ inline FastDiv fast_div(uint32_t d) {
 
 // Rotary positions of q and k ([batch][seq][heads][head_dim] by strides);
 // table: rot / 2 turn fractions, then the amplitude (bits of a float in the low
-// word).  inverse: by the negative angle.  positions NULL: start + t.
+// word).  inverse: by the negative angle.  positions NULL: start + start_t t.
 struct RopeArgs {
   const void* x[2]; void* y[2];          // q and k
   int64_t xs[2][3], ys[2][3];            // batch, position, head
   int heads[2];
   int batch, seq, dim, rot;
   const int32_t* positions; int64_t pos_b, pos_t;
-  int64_t start, start_t;                // position start + start_t t where positions is NULL
+  int64_t start, start_t;
   const uint64_t* table;
   int interleaved, inverse;
 };

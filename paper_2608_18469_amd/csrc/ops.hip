@@ -18,10 +18,11 @@ namespace {
 
 // hipLaunchKernel's own result (not the last error of any earlier call).
 template <typename A>
-hipError_t launch1(void (*kernel)(A), int64_t grid, int block, const A& a, hipStream_t s) {
+hipError_t launch1(void (*kernel)(A), int64_t grid, int block, const A& a, hipStream_t s, uint32_t grid_y = 1) {
   A copy = a;
   void* args[] = {&copy};
-  return hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3((uint32_t)grid), dim3((uint32_t)block), args, 0, s);
+  return hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3((uint32_t)grid, grid_y), dim3((uint32_t)block), args,
+                         0, s);
 }
 
 // Eight bf16 or four fp32 consecutive elements, moved by one 16-byte access from
@@ -60,22 +61,35 @@ __device__ __forceinline__ Chunk<T> ld_chunk(const T* p, int n) {
   return c;
 }
 template <typename T>
-__device__ __forceinline__ void st_chunk(T* p, int n, const float v[Chunk<T>::V]) {
-  if (n >= Chunk<T>::V) {
-    u32x4_t r;
+__device__ __forceinline__ Chunk<T> pack_chunk(const float v[Chunk<T>::V]) {
+  Chunk<T> c;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      if constexpr (sizeof(T) == 4)
-        r[k] = __float_as_uint(v[k]);
-      else
-        r[k] = (uint32_t)f2bf(v[2 * k]) | ((uint32_t)f2bf(v[2 * k + 1]) << 16);
-    }
-    *reinterpret_cast<typename Chunk<T>::mem_t*>(p) = r;
+  for (int k = 0; k < 4; ++k) {
+    if constexpr (sizeof(T) == 4)
+      c.r[k] = __float_as_uint(v[k]);
+    else
+      c.r[k] = (uint32_t)f2bf(v[2 * k]) | ((uint32_t)f2bf(v[2 * k + 1]) << 16);
+  }
+  return c;
+}
+template <typename T>
+__device__ __forceinline__ void st_raw(T* p, int n, const Chunk<T>& c) {
+  if (n >= Chunk<T>::V) {
+    *reinterpret_cast<typename Chunk<T>::mem_t*>(p) = c.r;
   } else {
 #pragma unroll
     for (int k = 0; k < Chunk<T>::V - 1; ++k)
-      if (k < n) p[k] = cvt<T>(v[k]);
+      if (k < n) {
+        if constexpr (sizeof(T) == 4)
+          p[k] = __uint_as_float(c.r[k]);
+        else
+          p[k] = (T)(c.r[k >> 1] >> (16 * (k & 1)));
+      }
   }
+}
+template <typename T>
+__device__ __forceinline__ void st_chunk(T* p, int n, const float v[Chunk<T>::V]) {
+  st_raw(p, n, pack_chunk<T>(v));
 }
 
 // Sum over groups of L = 16 or 64 lanes, the same bits in every lane: within 16
@@ -132,39 +146,135 @@ __global__ __launch_bounds__(kRopeFill) void ops_rope_fill(RopeFillArgs a) {
 
 hipError_t launch_rope_fill(const RopeFillArgs& a, hipStream_t s) { return launch1(ops_rope_fill, 1, kRopeFill, a, s); }
 
-// One token per workgroup; a thread takes pairs and passed columns in turn.
-template <typename T>
-__global__ __launch_bounds__(256) void ops_rope(RopeArgs a) {
-  const int half = a.rot / 2, units = a.dim - half;  // pairs, then columns that pass
+// A workgroup takes `tokens` consecutive positions of a batch row: it computes
+// their sines and cosines once into LDS, then its threads take units of those
+// tokens' heads, 32 bytes each: V pairs (two 16-byte chunks) or 2 V columns that
+// pass.  HBM bounds it: 671 MB read and written (32768 tokens of 40 heads of 128,
+// half of each turned) take 131 us, 5.1 TB/s.  Columns that pass in units of one
+// chunk, on a path of their own, took 163 us; several units' loads issued before
+// the sines 162 to 224 (the registers cost more waves than the loads hide).
+constexpr int kRopePairs = 2048;  // pairs of a workgroup's tokens (16 KB of LDS)
+struct RopePlan {
+  RopeArgs a;
+  FastDiv per_token, per_head, pairs;  // units of a token, of a head; pairs of a head
+  int turn;                            // units of a head that turn (the others pass)
+  int tokens;
+  uint32_t row_groups, groups;         // groups of tokens in a batch row, in all
+  int whole;  // the last unit ends with the columns it is for, overlapping the one before (not in place)
+};
+
+namespace {
+
+__device__ __forceinline__ uint32_t quotient(uint32_t n, const FastDiv& d) {
+  const uint32_t t = __umulhi(d.m, n);
+  return (t + ((n - t) >> d.s1)) >> d.s2;
+}
+
+}  // namespace
+
+template <typename T, bool INTER>
+__global__ __launch_bounds__(256) void ops_rope(RopePlan p) {
+  constexpr int V = Chunk<T>::V;
+  __shared__ float2 cs[kRopePairs + V];  // read to the end of a chunk
+  const RopeArgs& a = p.a;
+  const int half = a.rot / 2;
   const float amp = __uint_as_float((uint32_t)a.table[half]);
-  for (int64_t n = blockIdx.x; n < (int64_t)a.batch * a.seq; n += gridDim.x) {
-    const int b = (int)(n / a.seq), t = (int)(n % a.seq);
-    const int64_t p = rope_position(a, b, t);
-    for (int u = threadIdx.x; u < (a.heads[0] + a.heads[1]) * units; u += 256) {
-      int h = u / units;
-      const int i = u % units, w = h >= a.heads[0];
-      if (w) h -= a.heads[0];
-      const T* x = static_cast<const T*>(a.x[w]) + b * a.xs[w][0] + t * a.xs[w][1] + h * a.xs[w][2];
-      T* y = static_cast<T*>(a.y[w]) + b * a.ys[w][0] + t * a.ys[w][1] + h * a.ys[w][2];
-      if (i >= half) {
-        y[half + i] = x[half + i];
-        continue;
-      }
+  for (uint32_t g = blockIdx.x; g < p.groups; g += gridDim.x) {
+    const int b = (int)(g / p.row_groups), t0 = (int)(g % p.row_groups) * p.tokens;
+    const int tokens = min(p.tokens, a.seq - t0);
+    const uint32_t units = (uint32_t)tokens * p.per_token.d;
+    if (g != blockIdx.x) __syncthreads();  // the last group's sines have been read
+    for (uint32_t j = threadIdx.x; j < (uint32_t)(tokens * half); j += 256) {
+      const uint32_t tok = quotient(j, p.pairs);
+      const int64_t pos = rope_position(a, b, t0 + (int)tok);
       float s, c;
-      sincos_turn((uint64_t)p * a.table[i], s, c);
-      s *= a.inverse ? -amp : amp;
-      c *= amp;
-      const int i1 = a.interleaved ? 2 * i : i, i2 = a.interleaved ? 2 * i + 1 : half + i;
-      const float x1 = ldf(x + i1), x2 = ldf(x + i2);
-      y[i1] = cvt<T>(fmaf(x1, c, -(x2 * s)));
-      y[i2] = cvt<T>(fmaf(x2, c, x1 * s));
+      sincos_turn((uint64_t)pos * a.table[j - tok * half], s, c);
+      cs[j] = make_float2(c * amp, a.inverse ? -(s * amp) : s * amp);
+    }
+    __syncthreads();
+    for (uint32_t id = blockIdx.y * 256 + threadIdx.x; id < units; id += 256 * gridDim.y) {
+      const uint32_t tok = quotient(id, p.per_token), in_tok = id - tok * p.per_token.d;
+      const uint32_t hh = quotient(in_tok, p.per_head), c = in_tok - hh * p.per_head.d;
+      const int w = hh >= (uint32_t)a.heads[0], h = (int)hh - (w ? a.heads[0] : 0);
+      const int64_t t = t0 + (int64_t)tok;
+      const T* x = static_cast<const T*>(w ? a.x[1] : a.x[0]) + b * (w ? a.xs[1][0] : a.xs[0][0]) +
+                   t * (w ? a.xs[1][1] : a.xs[0][1]) + h * (w ? a.xs[1][2] : a.xs[0][2]);
+      T* y = static_cast<T*>(w ? a.y[1] : a.y[0]) + b * (w ? a.ys[1][0] : a.ys[0][0]) +
+             t * (w ? a.ys[1][1] : a.ys[0][1]) + h * (w ? a.ys[1][2] : a.ys[0][2]);
+      const bool turns = (int)c < p.turn;
+      // 2 V columns of a head: V pairs, or columns behind rot
+      const int end = turns ? a.rot : a.dim - a.rot;
+      int i = (turns ? (int)c : (int)c - p.turn) * 2 * V;
+      if (p.whole && end >= 2 * V) i = min(i, end - 2 * V);
+      const int left = min(2 * V, end - i);
+      int n1 = min(V, left), n2 = left - n1, second = V, at = (turns ? 0 : a.rot) + i;
+      if (!INTER && turns) {
+        n1 = n2 = left / 2;
+        second = half;
+        at = i / 2;
+      }
+      x += at;
+      y += at;
+      Chunk<T> x1 = ld_chunk(x, n1), x2 = ld_chunk(x + second, n2);
+      if (turns) {
+        const float2* q = cs + (int)tok * half + i / 2;
+        float o1[V], o2[V];
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+          if constexpr (INTER) {  // pair k is columns 2 k, 2 k + 1 of the two chunks in a row
+            const float v1 = 2 * k < V ? x1[2 * k] : x2[2 * k - V];
+            const float v2 = 2 * k < V ? x1[2 * k + 1] : x2[2 * k + 1 - V];
+            const float w1 = fmaf(v1, q[k].x, -(v2 * q[k].y)), w2 = fmaf(v2, q[k].x, v1 * q[k].y);
+            (2 * k < V ? o1[2 * k] : o2[2 * k - V]) = w1;
+            (2 * k < V ? o1[2 * k + 1] : o2[2 * k + 1 - V]) = w2;
+          } else {
+            o1[k] = fmaf(x1[k], q[k].x, -(x2[k] * q[k].y));
+            o2[k] = fmaf(x2[k], q[k].x, x1[k] * q[k].y);
+          }
+        }
+        x1 = pack_chunk<T>(o1);
+        x2 = pack_chunk<T>(o2);
+      }
+      st_raw(y, n1, x1);
+      st_raw(y + second, n2, x2);
     }
   }
 }
 
-hipError_t launch_rope(int bf16, const RopeArgs& a, hipStream_t s) {
-  const int64_t n = std::min<int64_t>((int64_t)a.batch * a.seq, 1 << 20);
-  return launch1(bf16 ? ops_rope<uint16_t> : ops_rope<float>, n, 256, a, s);
+hipError_t launch_rope(int bf16, const RopeArgs& args, hipStream_t s) {
+  RopePlan p{};
+  RopeArgs& a = p.a = args;
+  if (a.seq == 1) {  // one token a row: the rows are the positions
+    a.seq = a.batch;
+    a.batch = 1;
+    for (int w = 0; w < 2; ++w) {
+      a.xs[w][1] = a.xs[w][0];
+      a.ys[w][1] = a.ys[w][0];
+    }
+    a.pos_t = a.pos_b;
+    a.start_t = 0;
+  }
+  const int V = bf16 ? 8 : 4, half = a.rot / 2;
+  const bool in_place = a.x[0] == a.y[0] || (a.heads[1] && a.x[1] == a.y[1]);
+  const bool all_in_place = a.x[0] == a.y[0] && (!a.heads[1] || a.x[1] == a.y[1]);
+  p.whole = !in_place;
+  p.turn = (half + V - 1) / V;
+  const int per_head = p.turn + (all_in_place ? 0 : (a.dim - a.rot + 2 * V - 1) / (2 * V));
+  const int per_token = per_head * (a.heads[0] + a.heads[1]);
+  p.per_head = fast_div((uint32_t)per_head);
+  p.per_token = fast_div((uint32_t)per_token);
+  p.pairs = fast_div((uint32_t)half);
+  // as many tokens as give every thread one unit (16384 tokens of 16 heads of 64
+  // in bf16: 17.2 us; with two or four units a thread 18.7), fewer where that
+  // leaves less than two workgroups a compute unit
+  p.tokens = std::max(1, std::min({256 / per_token, kRopePairs / half, a.seq}));
+  while (p.tokens > 1 && (int64_t)a.batch * ((a.seq + p.tokens - 1) / p.tokens) < 512) p.tokens = (p.tokens + 1) / 2;
+  p.row_groups = (uint32_t)((a.seq + p.tokens - 1) / p.tokens);
+  p.groups = (uint32_t)a.batch * p.row_groups;
+  const uint32_t grid = std::min<uint32_t>(p.groups, 1 << 20);
+  const uint32_t splits = (uint32_t)((per_token + 1023) / 1024);  // of one token's heads, beyond four units a thread
+  if (bf16) return launch1(a.interleaved ? ops_rope<uint16_t, true> : ops_rope<uint16_t, false>, grid, 256, p, s, splits);
+  return launch1(a.interleaved ? ops_rope<float, true> : ops_rope<float, false>, grid, 256, p, s, splits);
 }
 
 // ---------------------------------------------------------------------------
