@@ -280,59 +280,6 @@ hipError_t launch_rope(int bf16, const RopeArgs& args, hipStream_t s) {
 // ---------------------------------------------------------------------------
 // layer norm
 // ---------------------------------------------------------------------------
-namespace {
-
-// Sums of two values over a workgroup of 256 threads, in every thread.
-__device__ __forceinline__ void block_sum2(float& u, float& v) {
-  __shared__ float part[2][4];
-  const int wave = threadIdx.x >> 6;
-  u = wave_sum(u);
-  v = wave_sum(v);
-  __syncthreads();  // the last call's sums have been read
-  if ((threadIdx.x & 63) == 0) {
-    part[0][wave] = u;
-    part[1][wave] = v;
-  }
-  __syncthreads();
-  u = part[0][0] + part[0][1] + part[0][2] + part[0][3];
-  v = part[1][0] + part[1][1] + part[1][2] + part[1][3];
-}
-
-}  // namespace
-
-// One row per workgroup.
-template <typename T>
-__global__ __launch_bounds__(256) void ops_norm(NormArgs a) {
-  for (int64_t n = blockIdx.x; n < a.rows; n += gridDim.x) {
-    const T* x = static_cast<const T*>(a.x) + n * a.ldx;
-    T* y = static_cast<T*>(a.y) + n * a.ldy;
-    float s = 0.f, q = 0.f;
-    for (int c = threadIdx.x; c < a.cols; c += 256) s += ldf(x + c);
-    block_sum2(s, q);
-    const float mean = s / (float)a.cols;
-    q = 0.f;
-    for (int c = threadIdx.x; c < a.cols; c += 256) {
-      const float d = ldf(x + c) - mean;
-      q = fmaf(d, d, q);
-    }
-    s = 0.f;
-    block_sum2(s, q);
-    const float r = 1.f / sqrtf(q / (float)a.cols + a.eps);
-    if (threadIdx.x == 0) {
-      if (a.mean) a.mean[n] = mean;
-      if (a.rstd) a.rstd[n] = r;
-    }
-    for (int c = threadIdx.x; c < a.cols; c += 256) {
-      const float h = (ldf(x + c) - mean) * r;
-      y[c] = cvt<T>(fmaf(h, a.w ? a.w[c] : 1.f, a.b ? a.b[c] : 0.f));
-    }
-  }
-}
-
-hipError_t launch_norm(int bf16, const NormArgs& a, hipStream_t s) {
-  return launch1(bf16 ? ops_norm<uint16_t> : ops_norm<float>, std::min<int64_t>(a.rows, 1 << 20), 256, a, s);
-}
-
 // Layouts of the row kernels: a row is held by `lanes` threads (16 of a wave, a
 // wave, or W waves), K chunks of 16 bytes each, `groups` rows at a time in a
 // workgroup of 256 or 512 threads.
@@ -344,6 +291,118 @@ struct RowShape {
   static constexpr int threads = lanes * groups, cols = lanes * K * Chunk<T>::V;
   static constexpr bool ahead = cols / lanes < 32;  // the backward holds the next row as well (registers)
 };
+
+namespace {
+
+// Calls f with the shape that holds a row of `cols` elements: 16 lanes for the
+// narrowest rows, then a wave with 1 or 2 chunks a lane, then 4 waves, then 8.
+template <typename T, typename F>
+auto with_row_shape(int cols, F&& f) {
+  constexpr int V = Chunk<T>::V;
+  if (cols <= 16 * V) return f(RowShape<T, 16, 1, 1>());
+  if (cols <= 64 * V) return f(RowShape<T, 64, 1, 1>());
+  if (cols <= 128 * V) return f(RowShape<T, 64, 1, 2>());
+  if (cols <= 256 * V) return f(RowShape<T, 64, 4, 1>());
+  if (cols <= 512 * V) return f(RowShape<T, 64, 4, 2>());
+  if (cols <= 1024 * V) return f(RowShape<T, 64, 8, 2>());
+  if constexpr (V == 4)
+    if (cols > 2048 * V) return f(RowShape<T, 64, 8, 8>());
+  return f(RowShape<T, 64, 8, 4>());
+}
+
+// Elements c .. c + V - 1 of an fp32 vector of which `left` are there; `none`
+// where there is no vector.
+template <int V>
+__device__ __forceinline__ void ld_vector(const float* p, int c, int left, float none, float v[V]) {
+#pragma unroll
+  for (int k = 0; k < V; ++k) v[k] = none;
+  if (!p) return;
+  if (left >= V) {
+#pragma unroll
+    for (int j = 0; j < V / 4; ++j) {
+      const u32x4_t t = *reinterpret_cast<const u32x4_at4_t*>(p + c + 4 * j);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[4 * j + k] = __uint_as_float(t[k]);
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < V - 1; ++k)
+      if (k < left) v[k] = p[c + k];
+  }
+}
+
+}  // namespace
+
+// Forward: one row per row group, read once into registers; the mean, then the
+// variance of the centred row, two reductions that wait for one another.
+template <typename S>
+__global__ __launch_bounds__(S::threads) void ops_norm(NormArgs a) {
+  typedef typename S::T T;
+  constexpr int V = Chunk<T>::V, L = S::L, W = S::W, K = S::K;
+  __shared__ float sums[2][S::groups][W];
+  const int grp = threadIdx.x / S::lanes, pos = threadIdx.x % S::lanes;
+  const int64_t n = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * S::groups + grp;
+  const bool row = n < a.rows;
+  const float cols = (float)a.cols;
+  Chunk<T> x[K];
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < K; ++i) {
+    const int c = (pos + i * S::lanes) * V;
+    x[i] = ld_chunk(static_cast<const T*>(a.x) + n * a.ldx + c, row ? a.cols - c : 0);
+#pragma unroll
+    for (int k = 0; k < V; ++k) s += x[i][k];
+  }
+  auto total = [&](float v, int which) {
+    v = lane_sum<L>(v);
+    if constexpr (W > 1) {
+      if ((threadIdx.x & 63) == 0) sums[which][grp][pos >> 6] = v;
+      __syncthreads();
+      v = 0.f;
+#pragma unroll
+      for (int j = 0; j < W; ++j) v += sums[which][grp][j];
+    }
+    return v;
+  };
+  // (divided: the product with a rounded 1 / cols would not give a constant row its own value)
+  const float mean = total(s, 0) / cols;
+  float q = 0.f;
+#pragma unroll
+  for (int i = 0; i < K; ++i) {
+    const int left = a.cols - (pos + i * S::lanes) * V;
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+      const float d = k < left ? x[i][k] - mean : 0.f;
+      q = fmaf(d, d, q);
+    }
+  }
+  const float r = 1.f / sqrtf(total(q, 1) / cols + a.eps);
+  if (!row) return;
+  if (pos == 0) {
+    if (a.mean) a.mean[n] = mean;
+    if (a.rstd) a.rstd[n] = r;
+  }
+#pragma unroll
+  for (int i = 0; i < K; ++i) {
+    const int c = (pos + i * S::lanes) * V, left = a.cols - c;
+    if (left <= 0) continue;
+    float w[V], b[V], o[V];
+    ld_vector<V>(a.w, c, left, 1.f, w);
+    ld_vector<V>(a.b, c, left, 0.f, b);
+#pragma unroll
+    for (int k = 0; k < V; ++k) o[k] = fmaf((x[i][k] - mean) * r, w[k], b[k]);
+    st_chunk(static_cast<T*>(a.y) + n * a.ldy + c, left, o);
+  }
+}
+
+hipError_t launch_norm(int bf16, const NormArgs& a, hipStream_t s) {
+  // 2^32 threads in x are not launched: beyond 2^22 workgroups they run on over y
+  auto run = [&](auto sh) {
+    const int64_t n = (a.rows + sh.groups - 1) / sh.groups, x = std::min<int64_t>(n, 1 << 22);
+    return launch1(ops_norm<decltype(sh)>, x, sh.threads, a, s, (uint32_t)((n + x - 1) / x));
+  };
+  return bf16 ? with_row_shape<uint16_t>(a.cols, run) : with_row_shape<float>(a.cols, run);
+}
 
 namespace {
 
@@ -413,11 +472,9 @@ __global__ __launch_bounds__(S::threads) void ops_norm_bwd(NormBwdArgs a) {
 #pragma unroll
   for (int i = 0; i < K; ++i) {
     const int c = (pos + i * S::lanes) * V;
+    ld_vector<V>(a.w, c, a.cols - c, 1.f, w[i]);
 #pragma unroll
-    for (int k = 0; k < V; ++k) {
-      w[i][k] = a.w && c + k < a.cols ? a.w[c + k] : 1.f;
-      aw[i][k] = ab[i][k] = 0.f;
-    }
+    for (int k = 0; k < V; ++k) aw[i][k] = ab[i][k] = 0.f;
   }
   const float inv = 1.f / (float)a.cols;
   const int64_t step = (int64_t)gridDim.x * G;
@@ -476,26 +533,6 @@ __global__ __launch_bounds__(S::threads) void ops_norm_bwd(NormBwdArgs a) {
   if constexpr (G > 1) __syncthreads();
   st_norm_part<S>(ab, comb, grp, pos, a.cols, part + a.ldpart);
 }
-
-namespace {
-
-// Calls f with the shape that holds a row of `cols` elements: 16 lanes for the
-// narrowest rows, then a wave with 1 or 2 chunks a lane, then 4 waves, then 8.
-template <typename T, typename F>
-auto with_row_shape(int cols, F&& f) {
-  constexpr int V = Chunk<T>::V;
-  if (cols <= 16 * V) return f(RowShape<T, 16, 1, 1>());
-  if (cols <= 64 * V) return f(RowShape<T, 64, 1, 1>());
-  if (cols <= 128 * V) return f(RowShape<T, 64, 1, 2>());
-  if (cols <= 256 * V) return f(RowShape<T, 64, 4, 1>());
-  if (cols <= 512 * V) return f(RowShape<T, 64, 4, 2>());
-  if (cols <= 1024 * V) return f(RowShape<T, 64, 8, 2>());
-  if constexpr (V == 4)
-    if (cols > 2048 * V) return f(RowShape<T, 64, 8, 8>());
-  return f(RowShape<T, 64, 8, 4>());
-}
-
-}  // namespace
 
 // Partial rows: one per workgroup, as many workgroups as the chip holds at
 // once at two per compute unit.
@@ -574,33 +611,68 @@ __device__ __forceinline__ void philox(uint32_t x[4], uint32_t k0, uint32_t k1) 
 
 }  // namespace
 
-// A thread takes groups of eight columns of a row.
+// A thread takes eight columns of a row: one counter, one or two chunks.  The
+// ten rounds are 20 products of 32 x 32 bits, which issue at a quarter of the
+// rate of an addition: 16 bits an element (rather than 32) keep them below the
+// time HBM needs.
+struct DropPlan {
+  DropArgs a;
+  FastDiv groups;  // eights of a row
+  uint32_t total;
+};
 template <typename T>
-__global__ __launch_bounds__(256) void ops_dropout(DropArgs a) {
-  const uint64_t off = a.offset + (a.step ? *a.step : 0);
-  const int groups = (a.cols + 7) / 8;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < a.rows * groups; i += (int64_t)gridDim.x * 256) {
-    const int64_t n = i / groups;
-    const int g = (int)(i % groups);
-    uint32_t bits[4] = {(uint32_t)g, (uint32_t)(a.row0 + n), (uint32_t)off, (uint32_t)(off >> 32)};
-    philox(bits, (uint32_t)a.seed, (uint32_t)(a.seed >> 32));
-    const T* x = static_cast<const T*>(a.x) + n * a.ldx;
-    const T* res = a.res ? static_cast<const T*>(a.res) + n * a.ldres : nullptr;
-    T* y = static_cast<T*>(a.y) + n * a.ldy;
+__global__ __launch_bounds__(256) void ops_dropout(DropPlan p) {
+  const DropArgs& a = p.a;
+  constexpr int V = Chunk<T>::V;
+  const uint32_t id = blockIdx.x * 256 + threadIdx.x;
+  if (id >= p.total) return;
+  const uint32_t n = quotient(id, p.groups), g = id - n * p.groups.d;
+  const int c = (int)(8 * g), left = a.cols - c;
+  const T* x = static_cast<const T*>(a.x) + n * a.ldx + c;
+  const T* res = a.res ? static_cast<const T*>(a.res) + n * a.ldres + c : nullptr;
+  T* y = static_cast<T*>(a.y) + n * a.ldy + c;
+  Chunk<T> xv[8 / V], rv[8 / V];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const int c = 8 * g + k;
-      if (c >= a.cols) break;
-      const uint32_t u = (bits[k >> 1] >> (16 * (k & 1))) & 0xffffu;
-      const float v = u >= a.limit ? ldf(x + c) * a.scale : 0.f;
-      y[c] = cvt<T>(res ? v + ldf(res + c) : v);
+  for (int j = 0; j < 8 / V; ++j) {
+    xv[j] = ld_chunk(x + j * V, left - j * V);
+    rv[j].r = u32x4_t{0u, 0u, 0u, 0u};
+    if (res) rv[j] = ld_chunk(res + j * V, left - j * V);
+  }
+  const uint64_t off = a.offset + (a.step ? *a.step : 0);
+  uint32_t bits[4] = {g, (uint32_t)a.row0 + n, (uint32_t)off, (uint32_t)(off >> 32)};
+  philox(bits, (uint32_t)a.seed, (uint32_t)(a.seed >> 32));
+#pragma unroll
+  for (int j = 0; j < 8 / V; ++j) {
+    float o[V];
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+      const int e = j * V + k;
+      const uint32_t u = e & 1 ? bits[e >> 1] >> 16 : bits[e >> 1] & 0xffffu;
+      o[k] = u >= a.limit ? xv[j][k] * a.scale : 0.f;
+      if (res) o[k] += rv[j][k];
     }
+    st_chunk(y + j * V, left - j * V, o);
   }
 }
 
-hipError_t launch_dropout(int bf16, const DropArgs& a, hipStream_t s) {
-  const int64_t n = (a.rows * ((a.cols + 7) / 8) + 255) / 256;
-  return launch1(bf16 ? ops_dropout<uint16_t> : ops_dropout<float>, std::min<int64_t>(n, 1 << 20), 256, a, s);
+hipError_t launch_dropout(int bf16, const DropArgs& args, hipStream_t s) {
+  DropPlan p{};
+  p.a = args;
+  p.groups = fast_div((uint32_t)((args.cols + 7) / 8));
+  // threads are numbered in 32 bits: that many rows a launch
+  const int64_t slab = std::max<int64_t>(1, (int64_t(1) << 31) / p.groups.d);
+  for (int64_t r = 0; r < args.rows; r += slab) {
+    const size_t size = bf16 ? 2 : 4;
+    p.a.row0 = args.row0 + r;
+    p.a.rows = std::min(slab, args.rows - r);
+    p.a.x = static_cast<const char*>(args.x) + size * r * args.ldx;
+    if (args.res) p.a.res = static_cast<const char*>(args.res) + size * r * args.ldres;
+    p.a.y = static_cast<char*>(args.y) + size * r * args.ldy;
+    p.total = (uint32_t)p.a.rows * p.groups.d;
+    const hipError_t e = launch1(bf16 ? ops_dropout<uint16_t> : ops_dropout<float>, (p.total + 255) / 256, 256, p, s);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace erase

@@ -504,6 +504,21 @@ def test_dropout_of_more_than_2_to_the_32_elements():
         assert np.array_equal(x[r].float().cpu().numpy() > 0, words[0]), r
 
 
+def test_layer_norm_of_more_rows_than_one_grid_row_takes():
+    """2^26 + 5 rows, a wave each: 2^32 threads and more."""
+    import torch
+    R, C = (1 << 26) + 5, 129
+    x = torch.zeros((R, C), dtype=torch.bfloat16, device="cuda")
+    at = [0, 1, 4 << 22, (1 << 26) - 1, 1 << 26, R - 1]
+    x[at] = torch.randn((len(at), C), device="cuda").bfloat16()
+    xr = _np(x[at])
+    print("[many rows]", R, C, flush=True)
+    ops.layer_norm(x, out=(x, None, None))
+    want, m, r = oo.layer_norm(xr)
+    assert (np.abs(_np(x[at]) - want) - _norm_bounds(xr, None, None, m, r, want, "bf16", C, 1e-5)[0]).max() <= 0
+    assert int(torch.count_nonzero(x[2:1000])) == 0 and int(torch.count_nonzero(x[-1000:-5])) <= C
+
+
 def test_two_streams_at_once():
     import torch
     x = torch.randn((4000, 512), device="cuda").bfloat16()
