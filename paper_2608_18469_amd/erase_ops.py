@@ -12,7 +12,10 @@ current stream), returns without waiting, and allocates the outputs that
 from __future__ import annotations
 
 import ctypes
+import struct
 from ctypes import POINTER, c_double, c_float, c_int32, c_int64, c_size_t, c_uint64, c_void_p
+
+import torch
 
 from . import erase
 from .erase import BF16, ERR_INVALID_ARG, ERR_SHAPE, ERR_WORKSPACE, F32, OK, EraseError
@@ -47,18 +50,23 @@ class DropoutConfig(ctypes.Structure):
                 ("offset", c_uint64), ("x_ld", c_int64), ("res_ld", c_int64), ("y_ld", c_int64)]
 
 
+# The same three as packed bytes, for the calls themselves: a Structure with its
+# arrays costs 2 us more than one pack, of 8 to 12 us for a whole call.
+_ROPE, _NORM, _DROPOUT = struct.Struct("8i14q"), struct.Struct("qiif5q"), struct.Struct("qqidQQ3q")
+assert (_ROPE.size, _NORM.size, _DROPOUT.size) == tuple(map(ctypes.sizeof, (RopeConfig, NormConfig, DropoutConfig)))
+
 # every entry point of include/erase_ops.h with its ctypes signature
 SIGNATURES = {
     "erase_rope_frequencies": (c_int32, [POINTER(RopeSpec), POINTER(c_double), POINTER(c_double)]),
     "erase_rope_table_bytes": (c_int32, [POINTER(RopeSpec), POINTER(c_size_t)]),
     "erase_rope_table": (c_int32, [POINTER(RopeSpec), c_void_p, c_void_p]),
-    "erase_rope": (c_int32, [POINTER(RopeConfig)] + [c_void_p] * 7),
-    "erase_rope_backward": (c_int32, [POINTER(RopeConfig)] + [c_void_p] * 7),
-    "erase_layer_norm": (c_int32, [POINTER(NormConfig)] + [c_void_p] * 7),
-    "erase_layer_norm_backward_scratch_bytes": (c_int32, [POINTER(NormConfig), POINTER(c_size_t)]),
-    "erase_layer_norm_backward": (c_int32, [POINTER(NormConfig)] + [c_void_p] * 10 + [c_size_t, c_void_p]),
-    "erase_dropout": (c_int32, [POINTER(DropoutConfig)] + [c_void_p] * 5),
-    "erase_dropout_backward": (c_int32, [POINTER(DropoutConfig)] + [c_void_p] * 4),
+    "erase_rope": (c_int32, [c_void_p] * 8),
+    "erase_rope_backward": (c_int32, [c_void_p] * 8),
+    "erase_layer_norm": (c_int32, [c_void_p] * 8),
+    "erase_layer_norm_backward_scratch_bytes": (c_int32, [c_void_p, POINTER(c_size_t)]),
+    "erase_layer_norm_backward": (c_int32, [c_void_p] * 11 + [c_size_t, c_void_p]),
+    "erase_dropout": (c_int32, [c_void_p] * 6),
+    "erase_dropout_backward": (c_int32, [c_void_p] * 5),
 }
 
 _lib = None
@@ -81,23 +89,28 @@ def _check(status: int, where: str):
         raise EraseError(status, where)
 
 
+_DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
+# the raw handle and number behind torch.cuda.current_stream() and current_device(), without an object a call
+_current_stream = (getattr(torch._C, "_cuda_getCurrentRawStream", None)
+                   or (lambda d: torch.cuda.current_stream(d).cuda_stream))
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
 def _dtype(where: str, name: str, t) -> int:
-    import torch
-    if t.dtype == torch.bfloat16:
-        return BF16
-    if t.dtype == torch.float32:
-        return F32
-    raise EraseError(ERR_INVALID_ARG, where, f"{name} must be float32 or bfloat16")
+    dt = _DTYPES.get(t.dtype)
+    if dt is None:
+        raise EraseError(ERR_INVALID_ARG, where, f"{name} must be float32 or bfloat16")
+    return dt
 
 
-def _on(where: str, x, **others):
-    """Every tensor on x's GPU."""
-    if not x.is_cuda:
+def _on(where: str, *tensors) -> int:
+    """The GPU that holds every tensor (None: not given)."""
+    dev = tensors[0].get_device()
+    if dev < 0:
         raise EraseError(ERR_INVALID_ARG, where, "tensors must be on the GPU")
-    dev = x.get_device()
-    for name, t in others.items():
+    for t in tensors:
         if t is not None and t.get_device() != dev:
-            raise EraseError(ERR_INVALID_ARG, where, f"{name} is not on the GPU of the other tensors")
+            raise EraseError(ERR_INVALID_ARG, where, "tensors are on different devices")
     return dev
 
 
@@ -108,25 +121,45 @@ def _like(where: str, name: str, t, x):
 
 
 def _vector(where: str, name: str, t, n: int):
-    import torch
-    if t is not None and (t.dtype != torch.float32 or t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1)):
+    if t is not None and (t.dtype != torch.float32 or t.shape != (n,) or not t.is_contiguous()):
         raise EraseError(ERR_INVALID_ARG, where, f"{name} must be a contiguous float32 tensor of {n}")
 
 
 def _run(where: str, fn, dev: int, stream, *args):
     """fn(*args, stream handle) with dev as the current device."""
-    import torch
-    if stream is not None and stream.device.index != dev:
+    if stream is None:
+        handle = _current_stream(dev)
+    elif stream.device.index == dev:
+        handle = stream.cuda_stream
+    else:
         raise EraseError(ERR_INVALID_ARG, where, "stream is not one of the tensors' GPU")
-    if dev == torch.cuda.current_device():
-        _check(fn(*args, (stream or torch.cuda.current_stream(dev)).cuda_stream), where)
-        return
-    with torch.cuda.device(dev):
-        _check(fn(*args, (stream or torch.cuda.current_stream(dev)).cuda_stream), where)
+    if dev == _current_device():
+        status = fn(*args, handle)
+    else:
+        with torch.cuda.device(dev):
+            status = fn(*args, handle)
+    if status != OK:
+        raise EraseError(status, where)
 
 
 def _ptr(t):
     return None if t is None else t.data_ptr()
+
+
+def _pack(where: str, form: struct.Struct, *values) -> bytes:
+    try:
+        return form.pack(*values)
+    except (struct.error, OverflowError) as e:
+        raise EraseError(ERR_SHAPE, where, str(e)) from None
+
+
+def _empty(shape, dtype, device, stream):
+    """Memory of the stream that will use it: a block of another stream's could
+    still be read or written there."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
 
 
 # ---------------------------------------------------------------------------
@@ -157,55 +190,59 @@ def rope_table(rot_dim, base=10000.0, scaling="none", factor=1.0, original_lengt
                stream=None) -> RopeTable:
     """The table of a rotation (erase_rope_spec's fields) on `device` (default: the
     current GPU), filled on `stream`; calls on another stream wait for it."""
-    import torch
     spec = _rope_spec(rot_dim, base, scaling, factor, original_length, fast, slow)
     n = c_size_t(0)
     _check(lib().erase_rope_table_bytes(ctypes.byref(spec), ctypes.byref(n)), "erase_rope_table_bytes")
     if not torch.cuda.is_available():
         raise RuntimeError("no HIP device available: the operators run only on the GPU")
     dev = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
-    data = torch.empty(n.value // 8, dtype=torch.int64, device=dev)
+    data = _empty(n.value // 8, torch.int64, dev, stream)
     _run("erase_rope_table", lib().erase_rope_table, data.get_device(), stream, ctypes.byref(spec), data.data_ptr())
     return RopeTable(spec, data)
 
 
+def _heads(where, name, t):
+    """Strides of [batch][seq][heads][head_dim] with contiguous columns."""
+    st = t.stride()
+    if len(st) != 4 or (st[3] != 1 and t.shape[3] > 1):
+        raise EraseError(ERR_SHAPE, where, f"{name} must be [batch][seq][heads][head_dim] with contiguous columns")
+    return st
+
+
 def _rotate(where, fn, q, k, table, positions, start, layout, out, stream):
-    import torch
-    if layout not in LAYOUTS:
+    lay = LAYOUTS.get(layout)
+    if lay is None:
         raise EraseError(ERR_INVALID_ARG, where, f"layout must be one of {sorted(LAYOUTS)}")
-    for name, t in (("q", q), ("k", k)):
-        if t is not None and (t.dim() != 4 or (t.shape[3] > 1 and t.stride(3) != 1)):
-            raise EraseError(ERR_SHAPE, where, f"{name} must be [batch][seq][heads][head_dim] with contiguous columns")
-    B, T, Hq, D = q.shape
+    qs = _heads(where, "q", q)
+    B, T, Hq, D = shape = q.shape
     dt = _dtype(where, "q", q)
-    if k is not None and (k.dtype != q.dtype or k.shape[:2] != q.shape[:2] or k.shape[3] != D):
-        raise EraseError(ERR_SHAPE, where, "k must have q's type, batch, length and head size")
-    dev = _on(where, q, k=k, table=table.data, positions=positions)
+    Hk, ks = 0, (0, 0, 0, 0)
+    if k is not None:
+        ks = _heads(where, "k", k)
+        Bk, Tk, Hk, Dk = k.shape
+        if k.dtype != q.dtype or Bk != B or Tk != T or Dk != D:
+            raise EraseError(ERR_SHAPE, where, "k must have q's type, batch, length and head size")
     pos_stride = 0
     if positions is not None:
-        if positions.dtype != torch.int32 or positions.shape != q.shape[:2] or (T > 1 and positions.stride(1) != 1):
+        ps = positions.stride()
+        if positions.dtype != torch.int32 or positions.shape != shape[:2] or (T > 1 and ps[1] != 1):
             raise EraseError(ERR_INVALID_ARG, where, "positions must be int32 [batch][seq] with unit stride along seq")
-        pos_stride = positions.stride(0)
+        pos_stride = ps[0]
     if out is None:
-        qo = torch.empty((B, T, Hq, D), dtype=q.dtype, device=q.device)
-        ko = None if k is None else torch.empty(k.shape, dtype=k.dtype, device=k.device)
+        qo = _empty(shape, q.dtype, q.device, stream)
+        ko = None if k is None else _empty(k.shape, k.dtype, k.device, stream)
     else:
         qo, ko = out
-        for name, o, t in (("out[0]", qo, q), ("out[1]", ko, k)):
-            if (o is None) != (t is None):
-                raise EraseError(ERR_INVALID_ARG, where, f"{name} must be given exactly where its input is")
-            if o is not None:
-                _like(where, name, o, t)
-                if D > 1 and o.stride(3) != 1:
-                    raise EraseError(ERR_SHAPE, where, f"{name} must have contiguous columns")
-        _on(where, q, out0=qo, out1=ko)
-    zero = (0, 0, 0, 0)
-    kh, ks, kos = (0, zero, zero) if k is None else (k.shape[2], k.stride(), ko.stride())
-    three = c_int64 * 3
-    cfg = RopeConfig(dt, LAYOUTS[layout], B, T, Hq, kh, D, table.rot_dim, three(*q.stride()[:3]), three(*ks[:3]),
-                     three(*qo.stride()[:3]), three(*kos[:3]), pos_stride, start)
-    _run(where, fn, dev, stream, ctypes.byref(cfg), q.data_ptr(), _ptr(k), qo.data_ptr(), _ptr(ko), _ptr(positions),
-         table.data.data_ptr())
+        if qo is None or (ko is None) != (k is None):
+            raise EraseError(ERR_INVALID_ARG, where, "out must give a tensor exactly where there is an input")
+        _like(where, "out[0]", qo, q)
+        if k is not None:
+            _like(where, "out[1]", ko, k)
+    dev = _on(where, q, k, table.data, positions, qo, ko)
+    qos = _heads(where, "out[0]", qo)
+    kos = ks if k is None else _heads(where, "out[1]", ko)
+    cfg = _pack(where, _ROPE, dt, lay, B, T, Hq, Hk, D, table.rot_dim, *qs[:3], *ks[:3], *qos[:3], *kos[:3], pos_stride, start)
+    _run(where, fn, dev, stream, cfg, q.data_ptr(), _ptr(k), qo.data_ptr(), _ptr(ko), _ptr(positions), table.data.data_ptr())
     return qo, ko
 
 
@@ -228,9 +265,12 @@ def rope_backward(dq, dk, table, positions=None, start=0, layout="half", out=Non
 # ---------------------------------------------------------------------------
 # layer norm
 # ---------------------------------------------------------------------------
-def _matrix(where: str, name: str, t):
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+def _matrix(where: str, name: str, t) -> int:
+    """The row pitch of [rows][cols] with unit column stride."""
+    st = t.stride()
+    if len(st) != 2 or (st[1] != 1 and t.shape[1] > 1):
         raise EraseError(ERR_SHAPE, where, f"{name} must be [rows][cols] with unit column stride")
+    return st[0]
 
 
 def layer_norm(x, weight=None, bias=None, eps=1e-5, out=None, stream=None):
@@ -238,44 +278,39 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, out=None, stream=None):
     bias float32 [cols] or None.  Returns (y, mean, rstd), the float32 statistics
     [rows] for the backward pass.  ``out`` gives the three; its statistics may be
     None (not computed), its y may be x."""
-    import torch
     where = "erase_layer_norm"
-    _matrix(where, "x", x)
+    ld = _matrix(where, "x", x)
     dt = _dtype(where, "x", x)
     R, C = x.shape
     _vector(where, "weight", weight, C)
     _vector(where, "bias", bias, C)
-    dev = _on(where, x, weight=weight, bias=bias)
     if out is None:
-        y = torch.empty((R, C), dtype=x.dtype, device=x.device)
-        mean, rstd = (torch.empty(R, dtype=torch.float32, device=x.device) for _ in range(2))
+        y = _empty((R, C), x.dtype, x.device, stream)
+        mean, rstd = _empty((2, R), torch.float32, x.device, stream)
     else:
         y, mean, rstd = out
         _like(where, "out[0]", y, x)
-        _matrix(where, "out[0]", y)
         _vector(where, "out[1]", mean, R)
         _vector(where, "out[2]", rstd, R)
-        _on(where, x, out0=y, out1=mean, out2=rstd)
-    cfg = NormConfig(R, C, dt, eps, x.stride(0), y.stride(0), 0, 0, 0)
-    _run(where, lib().erase_layer_norm, dev, stream, ctypes.byref(cfg), x.data_ptr(), _ptr(weight), _ptr(bias),
-         y.data_ptr(), _ptr(mean), _ptr(rstd))
+    dev = _on(where, x, weight, bias, y, mean, rstd)
+    cfg = _pack(where, _NORM, R, C, dt, eps, ld, _matrix(where, "out[0]", y), 0, 0, 0)
+    _run(where, lib().erase_layer_norm, dev, stream, cfg, x.data_ptr(), _ptr(weight), _ptr(bias), y.data_ptr(), _ptr(mean),
+         _ptr(rstd))
     return y, mean, rstd
 
 
-def _norm_scratch_bytes(cfg: NormConfig) -> int:
+def _norm_scratch_bytes(cfg: bytes) -> int:
     n = c_size_t(0)
-    _check(lib().erase_layer_norm_backward_scratch_bytes(ctypes.byref(cfg), ctypes.byref(n)),
-           "erase_layer_norm_backward_scratch_bytes")
+    _check(lib().erase_layer_norm_backward_scratch_bytes(cfg, ctypes.byref(n)), "erase_layer_norm_backward_scratch_bytes")
     return n.value
 
 
 def layer_norm_backward_scratch(x):
     """Scratch of layer_norm_backward() for tensors of x's shape and type; one for
     every call in flight."""
-    import torch
     where = "erase_layer_norm_backward"
     _matrix(where, "x", x)
-    cfg = NormConfig(x.shape[0], x.shape[1], _dtype(where, "x", x), 0.0, 0, 0, 0, 0, 0)
+    cfg = _pack(where, _NORM, x.shape[0], x.shape[1], _dtype(where, "x", x), 0.0, 0, 0, 0, 0, 0)
     return torch.empty(_norm_scratch_bytes(cfg), dtype=torch.uint8, device=x.device)
 
 
@@ -286,41 +321,47 @@ def layer_norm_backward(dy, x, weight, mean, rstd, residual=None, need_input=Tru
     x's shape, or None) is added to dx.  What is not needed is returned as None.
     ``out`` gives the three (dx may be dy or residual), ``scratch``
     layer_norm_backward_scratch()'s memory (allocated unless given)."""
-    import torch
     where = "erase_layer_norm_backward"
-    _matrix(where, "x", x)
+    ld = _matrix(where, "x", x)
     dt = _dtype(where, "x", x)
     R, C = x.shape
     _like(where, "dy", dy, x)
-    _matrix(where, "dy", dy)
     _vector(where, "weight", weight, C)
     _vector(where, "mean", mean, R)
     _vector(where, "rstd", rstd, R)
+    dx, dw, db = (None, None, None) if out is None else out
+    if not need_input:
+        dx = None
+    elif dx is None:
+        dx = _empty((R, C), x.dtype, x.device, stream)
+    else:
+        _like(where, "out[0]", dx, x)
+    if not need_weight:
+        dw = None
+    elif dw is None:
+        dw = _empty(C, torch.float32, x.device, stream)
+    else:
+        _vector(where, "out[1]", dw, C)
+    if not need_bias:
+        db = None
+    elif db is None:
+        db = _empty(C, torch.float32, x.device, stream)
+    else:
+        _vector(where, "out[2]", db, C)
     if residual is not None:
         _like(where, "residual", residual, x)
-        _matrix(where, "residual", residual)
-    dev = _on(where, x, dy=dy, weight=weight, mean=mean, rstd=rstd, residual=residual, scratch=scratch)
-    dx = dw = db = None
-    if out is not None:
-        dx, dw, db = out
-        if dx is not None:
-            _like(where, "out[0]", dx, x)
-            _matrix(where, "out[0]", dx)
-        _vector(where, "out[1]", dw, C)
-        _vector(where, "out[2]", db, C)
-        _on(where, x, out0=dx, out1=dw, out2=db)
-    dx = (dx if dx is not None else torch.empty((R, C), dtype=x.dtype, device=x.device)) if need_input else None
-    dw = (dw if dw is not None else torch.empty(C, dtype=torch.float32, device=x.device)) if need_weight else None
-    db = (db if db is not None else torch.empty(C, dtype=torch.float32, device=x.device)) if need_bias else None
-    cfg = NormConfig(R, C, dt, 0.0, x.stride(0), 0, dy.stride(0), 0 if dx is None else dx.stride(0),
-                     0 if residual is None else residual.stride(0))
-    if scratch is not None and not scratch.is_contiguous():
+    cfg = _pack(where, _NORM, R, C, dt, 0.0, ld, 0, _matrix(where, "dy", dy),
+                0 if dx is None else _matrix(where, "out[0]", dx),
+                0 if residual is None else _matrix(where, "residual", residual))
+    if scratch is None:
+        if need_weight or need_bias:
+            scratch = _empty(_norm_scratch_bytes(cfg), torch.uint8, x.device, stream)
+    elif not scratch.is_contiguous():
         raise EraseError(ERR_WORKSPACE, where, "scratch must be contiguous")
-    if scratch is None and (need_weight or need_bias):
-        scratch = torch.empty(_norm_scratch_bytes(cfg), dtype=torch.uint8, device=x.device)
-    _run(where, lib().erase_layer_norm_backward, dev, stream, ctypes.byref(cfg), x.data_ptr(), dy.data_ptr(), _ptr(weight),
+    dev = _on(where, x, dy, weight, mean, rstd, residual, dx, dw, db, scratch)
+    _run(where, lib().erase_layer_norm_backward, dev, stream, cfg, x.data_ptr(), dy.data_ptr(), _ptr(weight),
          _ptr(mean), _ptr(rstd), _ptr(residual), _ptr(dx), _ptr(dw), _ptr(db), _ptr(scratch),
-         0 if scratch is None else scratch.numel() * scratch.element_size())
+         0 if scratch is None else scratch.nbytes)
     return dx, dw, db
 
 
@@ -328,29 +369,27 @@ def layer_norm_backward(dy, x, weight, mean, rstd, residual=None, need_input=Tru
 # dropout
 # ---------------------------------------------------------------------------
 def _drop(where, fn, x, p, seed, offset, residual, step, out, stream):
-    import torch
-    _matrix(where, "x", x)
+    ld = _matrix(where, "x", x)
     dt = _dtype(where, "x", x)
-    if not 0 <= seed < 1 << 64 or not 0 <= offset < 1 << 64:
+    if not (0 <= seed < 1 << 64 and 0 <= offset < 1 << 64):
         raise EraseError(ERR_INVALID_ARG, where, "seed and offset must be 64-bit unsigned numbers")
-    if residual is not None:
-        _like(where, "residual", residual, x)
-        _matrix(where, "residual", residual)
     if step is not None and (step.dtype not in (torch.int64, torch.uint64) or step.numel() != 1):
         raise EraseError(ERR_INVALID_ARG, where, "step must be one int64 or uint64 on the device")
-    dev = _on(where, x, residual=residual, step=step, out=out)
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        out = _empty(x.shape, x.dtype, x.device, stream)
     else:
         _like(where, "out", out, x)
-        _matrix(where, "out", out)
-    cfg = DropoutConfig(x.shape[0], x.shape[1], dt, p, seed, offset, x.stride(0),
-                        0 if residual is None else residual.stride(0), out.stride(0))
+    lr = 0
+    if residual is not None:
+        _like(where, "residual", residual, x)
+        lr = _matrix(where, "residual", residual)
+    dev = _on(where, x, residual, step, out)
+    R, C = x.shape
+    cfg = _pack(where, _DROPOUT, R, C, dt, p, seed, offset, ld, lr, _matrix(where, "out", out))
     if fn == "erase_dropout":
-        args = (x.data_ptr(), _ptr(residual), out.data_ptr(), _ptr(step))
+        _run(where, lib().erase_dropout, dev, stream, cfg, x.data_ptr(), _ptr(residual), out.data_ptr(), _ptr(step))
     else:
-        args = (x.data_ptr(), out.data_ptr(), _ptr(step))
-    _run(where, getattr(lib(), fn), dev, stream, ctypes.byref(cfg), *args)
+        _run(where, lib().erase_dropout_backward, dev, stream, cfg, x.data_ptr(), out.data_ptr(), _ptr(step))
     return out
 
 
