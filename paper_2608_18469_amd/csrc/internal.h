@@ -430,8 +430,9 @@ struct NormArgs {
 hipError_t launch_norm(int bf16, const NormArgs& a, hipStream_t s);
 
 // Its backward: dx (nullable) and, over norm_bwd_parts() slices of the rows,
-// partial sums part[slice][0: dw, 1: db][ldpart] (part nullable), which
-// launch_norm_sum adds in order into dw and db (each nullable).
+// partial sums part[slice][0: dw, 1: db][ldpart] (part nullable: no sums
+// wanted), which launch_norm_sum adds in order into dw and db (each nullable).  A
+// single slice goes into dw and db at once.
 struct NormBwdArgs {
   const void* x; int64_t ldx;
   const void* dy; int64_t lddy;
@@ -439,6 +440,7 @@ struct NormBwdArgs {
   const void* res; int64_t ldres;
   void* dx; int64_t lddx;
   float* part; int64_t ldpart; int nparts;
+  float* dw; float* db;
   int64_t rows;
   int cols;
 };

@@ -281,21 +281,21 @@ hipError_t launch_rope(int bf16, const RopeArgs& args, hipStream_t s) {
 // layer norm
 // ---------------------------------------------------------------------------
 // Layouts of the row kernels: a row is held by `lanes` threads (16 of a wave, a
-// wave, or W waves), K chunks of 16 bytes each, `groups` rows at a time in a
-// workgroup of 256 or 512 threads.
+// wave, or W waves), K chunks of 16 bytes each; a workgroup of the forward takes
+// `groups` rows, one of the backward as many as 1024 threads hold.
 template <typename E, int Lanes, int Waves, int Chunks>
 struct RowShape {
   typedef E T;
   static constexpr int L = Lanes, W = Waves, K = Chunks;
-  static constexpr int lanes = L * W, groups = L == 16 ? 16 : W == 1 ? 4 : W == 4 ? 2 : 1;
-  static constexpr int threads = lanes * groups, cols = lanes * K * Chunk<T>::V;
-  static constexpr bool ahead = cols / lanes < 32;  // the backward holds the next row as well (registers)
+  static constexpr int lanes = L * W, cols = lanes * K * Chunk<T>::V;
+  static constexpr int groups = lanes < 256 ? 256 / lanes : 1, threads = lanes * groups;
+  static constexpr int bwd_groups = 1024 / lanes;
 };
 
 namespace {
 
 // Calls f with the shape that holds a row of `cols` elements: 16 lanes for the
-// narrowest rows, then a wave with 1 or 2 chunks a lane, then 4 waves, then 8.
+// narrowest rows, then a wave with 1 or 2 chunks a lane, then 4 waves, then 16.
 template <typename T, typename F>
 auto with_row_shape(int cols, F&& f) {
   constexpr int V = Chunk<T>::V;
@@ -304,10 +304,10 @@ auto with_row_shape(int cols, F&& f) {
   if (cols <= 128 * V) return f(RowShape<T, 64, 1, 2>());
   if (cols <= 256 * V) return f(RowShape<T, 64, 4, 1>());
   if (cols <= 512 * V) return f(RowShape<T, 64, 4, 2>());
-  if (cols <= 1024 * V) return f(RowShape<T, 64, 8, 2>());
+  if (cols <= 1024 * V) return f(RowShape<T, 64, 16, 1>());
   if constexpr (V == 4)
-    if (cols > 2048 * V) return f(RowShape<T, 64, 8, 8>());
-  return f(RowShape<T, 64, 8, 4>());
+    if (cols > 2048 * V) return f(RowShape<T, 64, 16, 4>());
+  return f(RowShape<T, 64, 16, 2>());
 }
 
 // Elements c .. c + V - 1 of an fp32 vector of which `left` are there; `none`
@@ -406,50 +406,28 @@ hipError_t launch_norm(int bf16, const NormArgs& a, hipStream_t s) {
 
 namespace {
 
-// A thread's part of x and dy of row n, and the row's statistics; zeros behind
-// the last row, which add nothing.
-template <typename S>
-struct NormRow {
-  Chunk<typename S::T> x[S::K], d[S::K];
-  float mean, r;
-};
-template <typename S>
-__device__ __forceinline__ NormRow<S> ld_norm_row(const NormBwdArgs& a, int64_t n, int pos) {
-  typedef typename S::T T;
-  NormRow<S> v;
-  const bool row = n < a.rows;
-  v.mean = row ? a.mean[n] : 0.f;
-  v.r = row ? a.rstd[n] : 0.f;
-#pragma unroll
-  for (int i = 0; i < S::K; ++i) {
-    const int c = (pos + i * S::lanes) * Chunk<T>::V;
-    const int left = row ? a.cols - c : 0;
-    v.x[i] = ld_chunk(static_cast<const T*>(a.x) + n * a.ldx + c, left);
-    v.d[i] = ld_chunk(static_cast<const T*>(a.dy) + n * a.lddy + c, left);
-  }
-  return v;
-}
-
-// A workgroup's sums of its rows' columns: row groups added in order in LDS.
+// A workgroup's sums of its rows' columns into `part` (NULL: not wanted), its
+// row groups added in order in LDS.
 template <typename S, typename A>
 __device__ __forceinline__ void st_norm_part(const A& acc, float* comb, int grp, int pos, int cols, float* part) {
   constexpr int V = Chunk<typename S::T>::V;
+  if (!part) return;
 #pragma unroll
   for (int i = 0; i < S::K; ++i)
 #pragma unroll
     for (int k = 0; k < V; ++k) {
       const int c = (pos + i * S::lanes) * V + k;
-      if constexpr (S::groups > 1)
+      if constexpr (S::bwd_groups > 1)
         comb[grp * S::cols + c] = acc[i][k];
       else if (c < cols)
         part[c] = acc[i][k];
     }
-  if constexpr (S::groups > 1) {
+  if constexpr (S::bwd_groups > 1) {
     __syncthreads();
-    for (int c = threadIdx.x; c < cols; c += S::threads) {
+    for (int c = threadIdx.x; c < cols; c += 1024) {
       float v = comb[c];
-#pragma unroll
-      for (int g = 1; g < S::groups; ++g) v += comb[g * S::cols + c];
+#pragma unroll 4
+      for (int g = 1; g < S::bwd_groups; ++g) v += comb[g * S::cols + c];
       part[c] = v;
     }
   }
@@ -458,13 +436,17 @@ __device__ __forceinline__ void st_norm_part(const A& acc, float* comb, int grp,
 }  // namespace
 
 // Backward.  A thread keeps its columns' weights and its partial sums of dw and
-// db in registers over all its rows; the loads of the next row are in flight
-// while the current one is reduced.  At the end the workgroup's row groups are
-// added in order through LDS, and one partial row per workgroup is stored.
+// db in registers over all its rows.  At the end the workgroup's row groups are
+// added in order through LDS and one partial row per workgroup is stored (a
+// single workgroup stores dw and db themselves).  Workgroups of 1024 threads, one
+// a compute unit, keep the partial rows few: 16384 x 512 bf16 with res takes 18.7
+// us with 256 of them, 23.3 with 512 of 256 threads, 31 with 256 of 256 (too few
+// rows in flight).  The next row's loads ahead of the reduction gain nothing over
+// the other waves' (18.8).
 template <typename S>
-__global__ __launch_bounds__(S::threads) void ops_norm_bwd(NormBwdArgs a) {
+__global__ __launch_bounds__(1024) void ops_norm_bwd(NormBwdArgs a) {
   typedef typename S::T T;
-  constexpr int V = Chunk<T>::V, G = S::groups, L = S::L, W = S::W, K = S::K;
+  constexpr int V = Chunk<T>::V, G = S::bwd_groups, L = S::L, W = S::W, K = S::K;
   __shared__ float2 sums[2][G][W];
   __shared__ float comb[G > 1 ? G * S::cols : 1];
   const int grp = threadIdx.x / S::lanes, pos = threadIdx.x % S::lanes;
@@ -477,21 +459,25 @@ __global__ __launch_bounds__(S::threads) void ops_norm_bwd(NormBwdArgs a) {
     for (int k = 0; k < V; ++k) aw[i][k] = ab[i][k] = 0.f;
   }
   const float inv = 1.f / (float)a.cols;
-  const int64_t step = (int64_t)gridDim.x * G;
-  int64_t n = (int64_t)blockIdx.x * G + grp;
-  NormRow<S> next;
-  if constexpr (S::ahead) next = ld_norm_row<S>(a, n, pos);
   int buf = 0;
   // the same number of rounds for every row group of the workgroup
-  for (int64_t n0 = (int64_t)blockIdx.x * G; n0 < a.rows; n0 += step, n += step) {
-    const NormRow<S> cur = S::ahead ? next : ld_norm_row<S>(a, n, pos);
-    if constexpr (S::ahead) next = ld_norm_row<S>(a, n + step, pos);
+  for (int64_t n0 = (int64_t)blockIdx.x * G; n0 < a.rows; n0 += (int64_t)gridDim.x * G) {
+    const int64_t n = n0 + grp;
+    const bool row = n < a.rows;  // behind the last row: zeros, which add nothing
+    const float mean = row ? a.mean[n] : 0.f, r = row ? a.rstd[n] : 0.f;
+    Chunk<T> x[K], d[K];
+#pragma unroll
+    for (int i = 0; i < K; ++i) {
+      const int c = (pos + i * S::lanes) * V, left = row ? a.cols - c : 0;
+      x[i] = ld_chunk(static_cast<const T*>(a.x) + n * a.ldx + c, left);
+      d[i] = ld_chunk(static_cast<const T*>(a.dy) + n * a.lddy + c, left);
+    }
     float sg = 0.f, sgh = 0.f;
 #pragma unroll
     for (int i = 0; i < K; ++i)
 #pragma unroll
       for (int k = 0; k < V; ++k) {
-        const float dv = cur.d[i][k], h = (cur.x[i][k] - cur.mean) * cur.r, g = dv * w[i][k];
+        const float dv = d[i][k], h = (x[i][k] - mean) * r, g = dv * w[i][k];
         sg += g;
         sgh = fmaf(g, h, sgh);
         aw[i][k] = fmaf(dv, h, aw[i][k]);
@@ -511,38 +497,43 @@ __global__ __launch_bounds__(S::threads) void ops_norm_bwd(NormBwdArgs a) {
       }
       buf ^= 1;  // one barrier a round: the round after next writes this buffer again
     }
-    if (n >= a.rows) continue;
+    if (!row) continue;
     const float mg = sg * inv, mgh = sgh * inv;
 #pragma unroll
     for (int i = 0; i < K; ++i) {
       const int c = (pos + i * S::lanes) * V;
       if (c >= a.cols) continue;
+      // g and h are unpacked again: held over the reduction they cost 2 K V registers
+      asm volatile("" : "+v"(x[i].r), "+v"(d[i].r));
       Chunk<T> res;
       res.r = u32x4_t{0u, 0u, 0u, 0u};
       if (a.res) res = ld_chunk(static_cast<const T*>(a.res) + n * a.ldres + c, a.cols - c);
       float o[V];
 #pragma unroll
-      for (int k = 0; k < V; ++k)
-        o[k] = fmaf(cur.r, cur.d[i][k] * w[i][k] - mg - (cur.x[i][k] - cur.mean) * cur.r * mgh, res[k]);
+      for (int k = 0; k < V; ++k) o[k] = fmaf(r, d[i][k] * w[i][k] - mg - (x[i][k] - mean) * r * mgh, res[k]);
       st_chunk(static_cast<T*>(a.dx) + n * a.lddx + c, a.cols - c, o);
     }
   }
   if (!a.part) return;
+  const bool alone = a.nparts == 1;
   float* part = a.part + (int64_t)blockIdx.x * 2 * a.ldpart;
-  st_norm_part<S>(aw, comb, grp, pos, a.cols, part);
+  st_norm_part<S>(aw, comb, grp, pos, a.cols, alone ? a.dw : part);
   if constexpr (G > 1) __syncthreads();
-  st_norm_part<S>(ab, comb, grp, pos, a.cols, part + a.ldpart);
+  st_norm_part<S>(ab, comb, grp, pos, a.cols, alone ? a.db : part + a.ldpart);
 }
 
-// Partial rows: one per workgroup, as many workgroups as the chip holds at
-// once at two per compute unit.
+// Partial rows: one per workgroup, a workgroup per compute unit; a single one
+// (and no second launch) while it takes at most two rounds of rows.
 int norm_bwd_parts(int bf16, int64_t rows, int cols) {
-  auto parts = [&](auto sh) { return (int)std::max<int64_t>(1, std::min<int64_t>((rows + sh.groups - 1) / sh.groups, 512)); };
+  auto parts = [&](auto sh) {
+    constexpr int g = decltype(sh)::bwd_groups;
+    return rows <= 2 * g ? 1 : (int)std::min<int64_t>((rows + g - 1) / g, 256);
+  };
   return bf16 ? with_row_shape<uint16_t>(cols, parts) : with_row_shape<float>(cols, parts);
 }
 
 hipError_t launch_norm_bwd(int bf16, const NormBwdArgs& a, hipStream_t s) {
-  auto run = [&](auto sh) { return launch1(ops_norm_bwd<decltype(sh)>, a.nparts, sh.threads, a, s); };
+  auto run = [&](auto sh) { return launch1(ops_norm_bwd<decltype(sh)>, a.nparts, 1024, a, s); };
   return bf16 ? with_row_shape<uint16_t>(a.cols, run) : with_row_shape<float>(a.cols, run);
 }
 
@@ -560,6 +551,7 @@ __global__ __launch_bounds__(256) void ops_norm_sum(NormSumArgs a) {
   const int slice = threadIdx.x >> 2;
   float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
   if (c < 2 * a.ldpart)
+#pragma unroll 4
     for (int g = slice; g < a.nparts; g += 64) {
       const float4 p = *reinterpret_cast<const float4*>(a.part + (int64_t)g * 2 * a.ldpart + c);
       v.x += p.x, v.y += p.y, v.z += p.z, v.w += p.w;

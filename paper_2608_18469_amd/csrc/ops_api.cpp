@@ -329,11 +329,13 @@ erase_status erase_layer_norm_backward(const erase_norm_config* cfg, const void*
     a.part = part;
     a.ldpart = ldp;
     a.nparts = nparts;
+    a.dw = dw;
+    a.db = db;
     a.rows = c.rows;
     a.cols = c.cols;
     if (launch_norm_bwd(bf16, a, s) != hipSuccess) return ERASE_ERR_HIP;
   }
-  return sums ? done(launch_norm_sum(part, ldp, nparts, c.cols, dw, db, s)) : ERASE_OK;
+  return sums && nparts != 1 ? done(launch_norm_sum(part, ldp, nparts, c.cols, dw, db, s)) : ERASE_OK;
 }
 
 erase_status erase_dropout(const erase_dropout_config* cfg, const void* x, const void* res, void* y,
