@@ -26,14 +26,20 @@ hipError_t launch1(void (*kernel)(A), int64_t grid, int block, const A& a, hipSt
 }
 
 // Eight bf16 or four fp32 consecutive elements, moved by one 16-byte access from
-// any element's address (the hardware splits what straddles a line), or one by
-// one where fewer than that are left.  Elements past the end are zero.
+// any element's address (the hardware splits what straddles a line).  Where
+// fewer are left they move in accesses of 8, 4 and 2 bytes, one for each binary
+// digit of their number: three independent loads instead of up to seven that
+// wait for one another.  Elements past the end are zero.
 typedef uint32_t u32x4_at2_t __attribute__((ext_vector_type(4), aligned(2)));
 typedef uint32_t u32x4_at4_t __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t u32x2_at2_t __attribute__((ext_vector_type(2), aligned(2)));
+typedef uint32_t u32x2_at4_t __attribute__((ext_vector_type(2), aligned(4)));
+typedef uint32_t u32_at2_t __attribute__((aligned(2)));
 template <typename T>
 struct Chunk {
   static constexpr int V = 16 / sizeof(T);
   typedef std::conditional_t<sizeof(T) == 2, u32x4_at2_t, u32x4_at4_t> mem_t;
+  typedef std::conditional_t<sizeof(T) == 2, u32x2_at2_t, u32x2_at4_t> mem2_t;
   u32x4_t r;
   __device__ __forceinline__ float operator[](int k) const {
     if constexpr (sizeof(T) == 4)
@@ -49,14 +55,27 @@ __device__ __forceinline__ Chunk<T> ld_chunk(const T* p, int n) {
     c.r = *reinterpret_cast<const typename Chunk<T>::mem_t*>(p);
   } else {
     c.r = u32x4_t{0u, 0u, 0u, 0u};
-#pragma unroll
-    for (int k = 0; k < Chunk<T>::V - 1; ++k)
-      if (k < n) {
-        if constexpr (sizeof(T) == 4)
-          c.r[k] = __float_as_uint(p[k]);
-        else
-          c.r[k >> 1] |= (uint32_t)p[k] << (16 * (k & 1));
+    if (n > 0) {
+      constexpr int E = 8 / sizeof(T);  // elements of 8 bytes
+      typename Chunk<T>::mem2_t two = {0u, 0u};
+      uint32_t one = 0u, half = 0u;
+      if (n & E) two = *reinterpret_cast<const typename Chunk<T>::mem2_t*>(p);
+      if constexpr (sizeof(T) == 4) {
+        if (n & 1) one = __float_as_uint(p[n & 2]);
+      } else {
+        if (n & 2) one = *reinterpret_cast<const u32_at2_t*>(p + (n & 4));
+        if (n & 1) half = p[n & 6];
       }
+      const bool front = !(n & E);  // the 4-byte word comes first
+      c.r[0] = front ? one : two[0];
+      c.r[1] = front ? 0u : two[1];
+      c.r[2] = front ? 0u : one;
+      if constexpr (sizeof(T) == 2) {
+        const int w = (n & 6) >> 1;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) c.r[k] |= k == w ? half : 0u;
+      }
+    }
   }
   return c;
 }
@@ -76,15 +95,17 @@ template <typename T>
 __device__ __forceinline__ void st_raw(T* p, int n, const Chunk<T>& c) {
   if (n >= Chunk<T>::V) {
     *reinterpret_cast<typename Chunk<T>::mem_t*>(p) = c.r;
-  } else {
-#pragma unroll
-    for (int k = 0; k < Chunk<T>::V - 1; ++k)
-      if (k < n) {
-        if constexpr (sizeof(T) == 4)
-          p[k] = __uint_as_float(c.r[k]);
-        else
-          p[k] = (T)(c.r[k >> 1] >> (16 * (k & 1)));
-      }
+  } else if (n > 0) {
+    constexpr int E = 8 / sizeof(T);
+    if (n & E) *reinterpret_cast<typename Chunk<T>::mem2_t*>(p) = typename Chunk<T>::mem2_t{c.r[0], c.r[1]};
+    const uint32_t one = n & E ? c.r[2] : c.r[0];
+    if constexpr (sizeof(T) == 4) {
+      if (n & 1) p[n & 2] = __uint_as_float(one);
+    } else {
+      if (n & 2) *reinterpret_cast<u32_at2_t*>(p + (n & 4)) = one;
+      const uint32_t next = n & E ? c.r[3] : c.r[1];
+      if (n & 1) p[n & 6] = (T)(n & 2 ? next : one);
+    }
   }
 }
 template <typename T>
@@ -283,10 +304,11 @@ hipError_t launch_rope(int bf16, const RopeArgs& args, hipStream_t s) {
 // Layouts of the row kernels: a row is held by `lanes` threads (16 of a wave, a
 // wave, or W waves), K chunks of 16 bytes each; a workgroup of the forward takes
 // `groups` rows, one of the backward as many as 1024 threads hold.
-template <typename E, int Lanes, int Waves, int Chunks>
+template <typename E, int Lanes, int Waves, int Chunks, bool Narrow = false>
 struct RowShape {
   typedef E T;
   static constexpr int L = Lanes, W = Waves, K = Chunks;
+  static constexpr bool narrow = Narrow;  // rows of less than a chunk
   static constexpr int lanes = L * W, cols = lanes * K * Chunk<T>::V;
   static constexpr int groups = lanes < 256 ? 256 / lanes : 1, threads = lanes * groups;
   static constexpr int bwd_groups = 1024 / lanes;
@@ -294,64 +316,153 @@ struct RowShape {
 
 namespace {
 
-// Calls f with the shape that holds a row of `cols` elements: 16 lanes for the
-// narrowest rows, then a wave with 1 or 2 chunks a lane, then 4 waves, then 16.
+// Calls f with the shape that holds a row of `cols` elements in the forward, and
+// in the backward (whose workgroups have 1024 threads).  The forward takes the
+// fewest waves that hold the row with weight and bias: rows of a wave need no
+// barrier (16000 x 1500 bf16: 21.5 us with 3 chunks a lane, 25.6 with 4 waves), and
+// several rows of a compute unit are in flight (3605 x 4160: 17.3 us with 4 waves
+// of 3 chunks, 25.5 with 16 of 1).  The backward holds three times as much a
+// column and takes one chunk a lane while it can.
 template <typename T, typename F>
-auto with_row_shape(int cols, F&& f) {
+auto with_norm_shape(int cols, F&& f) {
   constexpr int V = Chunk<T>::V;
+  if (cols < V) return f(RowShape<T, 16, 1, 1, true>());
   if (cols <= 16 * V) return f(RowShape<T, 16, 1, 1>());
   if (cols <= 64 * V) return f(RowShape<T, 64, 1, 1>());
   if (cols <= 128 * V) return f(RowShape<T, 64, 1, 2>());
+  if (cols <= 192 * V) return f(RowShape<T, 64, 1, 3>());
   if (cols <= 256 * V) return f(RowShape<T, 64, 4, 1>());
   if (cols <= 512 * V) return f(RowShape<T, 64, 4, 2>());
+  if (cols <= 768 * V) return f(RowShape<T, 64, 4, 3>());
+  if (cols <= 1024 * V) return f(RowShape<T, 64, 4, 4>());
+  if constexpr (V == 4)
+    if (cols > 2048 * V) return f(RowShape<T, 64, 16, 4>());
+  return f(RowShape<T, 64, 16, 2>());
+}
+template <typename T, typename F>
+auto with_norm_bwd_shape(int cols, F&& f) {
+  constexpr int V = Chunk<T>::V;
+  if (cols < V) return f(RowShape<T, 16, 1, 1, true>());
+  if (cols <= 16 * V) return f(RowShape<T, 16, 1, 1>());
+  if (cols <= 64 * V) return f(RowShape<T, 64, 1, 1>());
+  if (cols <= 128 * V) return f(RowShape<T, 64, 2, 1>());
+  if (cols <= 256 * V) return f(RowShape<T, 64, 4, 1>());
+  if (cols <= 512 * V) return f(RowShape<T, 64, 8, 1>());
   if (cols <= 1024 * V) return f(RowShape<T, 64, 16, 1>());
   if constexpr (V == 4)
     if (cols > 2048 * V) return f(RowShape<T, 64, 16, 4>());
   return f(RowShape<T, 64, 16, 2>());
 }
 
-// Elements c .. c + V - 1 of an fp32 vector of which `left` are there; `none`
-// where there is no vector.
-template <int V>
-__device__ __forceinline__ void ld_vector(const float* p, int c, int left, float none, float v[V]) {
+// The V columns that a thread's chunk i covers: [at, at + V), of which the first
+// `skip` belong to the chunk before.  A row's last chunk ends with the row, so
+// that every load is a whole one and none waits in a branch for the row's last
+// columns (0 to 7 of them); a thread behind the row skips all V.
+struct Window {
+  int at, skip;
+};
+template <typename S>
+__device__ __forceinline__ Window window(int pos, int i, int cols) {
+  constexpr int V = Chunk<typename S::T>::V;
+  const int c = (pos + i * S::lanes) * V, at = min(c, cols - V);
+  return {at, min(c - at, V)};
+}
+// Chunk i of every thread lies within the row: nothing to skip.
+template <typename S>
+__device__ __forceinline__ bool whole(int i, int cols) {
+  return (i + 1) * S::lanes * Chunk<typename S::T>::V <= cols;
+}
+// The V elements of a window (rows narrower than V: one by one).
+template <typename S, typename T>
+__device__ __forceinline__ Chunk<T> ld_window(const T* p, const Window& w) {
+  constexpr int V = Chunk<T>::V;
+  Chunk<T> c;
+  if constexpr (!S::narrow) {
+    c.r = *reinterpret_cast<const typename Chunk<T>::mem_t*>(p + w.at);
+  } else {
+    float v[V];
 #pragma unroll
-  for (int k = 0; k < V; ++k) v[k] = none;
+    for (int k = 0; k < V; ++k) v[k] = k >= w.skip ? ldf(p + w.at + k) : 0.f;
+    c = pack_chunk<T>(v);
+  }
+  return c;
+}
+// Zeros in the first `skip` elements.
+template <typename T>
+__device__ __forceinline__ void clear_front(Chunk<T>& c, int skip) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    if constexpr (sizeof(T) == 4)
+      c.r[k] = k >= skip ? c.r[k] : 0u;
+    else
+      c.r[k] &= 2 * k >= skip ? 0xffffffffu : 2 * k + 1 >= skip ? 0xffff0000u : 0u;
+  }
+}
+// V elements of an fp32 vector (none: `empty`).
+template <typename S, int V>
+__device__ __forceinline__ void ld_weights(const float* p, const Window& w, float empty, float (&v)[V]) {
+#pragma unroll
+  for (int k = 0; k < V; ++k) v[k] = empty;
   if (!p) return;
-  if (left >= V) {
+  if constexpr (!S::narrow) {
 #pragma unroll
     for (int j = 0; j < V / 4; ++j) {
-      const u32x4_t t = *reinterpret_cast<const u32x4_at4_t*>(p + c + 4 * j);
+      const u32x4_t t = *reinterpret_cast<const u32x4_at4_t*>(p + w.at + 4 * j);
 #pragma unroll
       for (int k = 0; k < 4; ++k) v[4 * j + k] = __uint_as_float(t[k]);
     }
   } else {
 #pragma unroll
-    for (int k = 0; k < V - 1; ++k)
-      if (k < left) v[k] = p[c + k];
+    for (int k = 0; k < V; ++k)
+      if (k >= w.skip) v[k] = p[w.at + k];
+  }
+}
+// Stores a window's own columns: all V, or the last ones by the binary digits of
+// their number.
+template <typename T>
+__device__ __forceinline__ void st_window(T* p, const Window& w, const float v[Chunk<T>::V]) {
+  constexpr int V = Chunk<T>::V, E = 8 / sizeof(T);
+  const Chunk<T> c = pack_chunk<T>(v);
+  const int n = V - w.skip;
+  T* end = p + w.at + V;
+  if (n == V) {
+    *reinterpret_cast<typename Chunk<T>::mem_t*>(end - V) = c.r;
+  } else if (n > 0) {
+    if (n & E) *reinterpret_cast<typename Chunk<T>::mem2_t*>(end - E) = typename Chunk<T>::mem2_t{c.r[2], c.r[3]};
+    const uint32_t one = n & E ? c.r[1] : c.r[3];
+    if constexpr (sizeof(T) == 4) {
+      if (n & 1) end[-(n & 2) - 1] = __uint_as_float(one);
+    } else {
+      if (n & 2) *reinterpret_cast<u32_at2_t*>(end - (n & 4) - 2) = one;
+      const uint32_t next = n & E ? c.r[0] : c.r[2];
+      if (n & 1) end[-(n & 6) - 1] = (T)((n & 2 ? next : one) >> 16);
+    }
   }
 }
 
 }  // namespace
 
-// Forward: one row per row group, read once into registers; the mean, then the
-// variance of the centred row, two reductions that wait for one another.
+constexpr int kNormGroups = 2048;  // workgroups of the forward, eight a compute unit
+
+// Forward: a row is read once into registers; the mean, then the variance of the
+// centred row, two reductions that wait for one another.  A workgroup takes many
+// rows, so that weight and bias (twice the bytes of a bf16 row each) are read
+// once per thread, not per row: 8000 x 4096 bf16 takes 27.7 us (4.7 TB/s), 34.9
+// with weight and bias read again for every row.
 template <typename S>
 __global__ __launch_bounds__(S::threads) void ops_norm(NormArgs a) {
   typedef typename S::T T;
   constexpr int V = Chunk<T>::V, L = S::L, W = S::W, K = S::K;
   __shared__ float sums[2][S::groups][W];
   const int grp = threadIdx.x / S::lanes, pos = threadIdx.x % S::lanes;
-  const int64_t n = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * S::groups + grp;
-  const bool row = n < a.rows;
   const float cols = (float)a.cols;
-  Chunk<T> x[K];
-  float s = 0.f;
+  float w[K][V], b[K][V];
+  Window at[K];
 #pragma unroll
   for (int i = 0; i < K; ++i) {
-    const int c = (pos + i * S::lanes) * V;
-    x[i] = ld_chunk(static_cast<const T*>(a.x) + n * a.ldx + c, row ? a.cols - c : 0);
-#pragma unroll
-    for (int k = 0; k < V; ++k) s += x[i][k];
+    at[i] = window<S>(pos, i, a.cols);
+    ld_weights<S>(a.w, at[i], 1.f, w[i]);
+    ld_weights<S>(a.b, at[i], 0.f, b[i]);
   }
   auto total = [&](float v, int which) {
     v = lane_sum<L>(v);
@@ -364,44 +475,64 @@ __global__ __launch_bounds__(S::threads) void ops_norm(NormArgs a) {
     }
     return v;
   };
-  // (divided: the product with a rounded 1 / cols would not give a constant row its own value)
-  const float mean = total(s, 0) / cols;
-  float q = 0.f;
+  // the same number of rounds for every row group of the workgroup
+  for (int64_t n0 = (int64_t)blockIdx.x * S::groups; n0 < a.rows; n0 += (int64_t)gridDim.x * S::groups) {
+    const bool row = n0 + grp < a.rows;
+    const int64_t n = row ? n0 + grp : n0;  // (behind the last row: an existing one, not stored)
+    Chunk<T> x[K];
 #pragma unroll
-  for (int i = 0; i < K; ++i) {
-    const int left = a.cols - (pos + i * S::lanes) * V;
-#pragma unroll
-    for (int k = 0; k < V; ++k) {
-      const float d = k < left ? x[i][k] - mean : 0.f;
-      q = fmaf(d, d, q);
+    for (int i = 0; i < K; ++i) {
+      x[i] = ld_window<S>(static_cast<const T*>(a.x) + n * a.ldx, at[i]);
     }
-  }
-  const float r = 1.f / sqrtf(total(q, 1) / cols + a.eps);
-  if (!row) return;
-  if (pos == 0) {
-    if (a.mean) a.mean[n] = mean;
-    if (a.rstd) a.rstd[n] = r;
-  }
+    float s = 0.f;
 #pragma unroll
-  for (int i = 0; i < K; ++i) {
-    const int c = (pos + i * S::lanes) * V, left = a.cols - c;
-    if (left <= 0) continue;
-    float w[V], b[V], o[V];
-    ld_vector<V>(a.w, c, left, 1.f, w);
-    ld_vector<V>(a.b, c, left, 0.f, b);
+    for (int i = 0; i < K; ++i) {
+      if (whole<S>(i, a.cols)) {
 #pragma unroll
-    for (int k = 0; k < V; ++k) o[k] = fmaf((x[i][k] - mean) * r, w[k], b[k]);
-    st_chunk(static_cast<T*>(a.y) + n * a.ldy + c, left, o);
+        for (int k = 0; k < V; ++k) s += x[i][k];
+      } else {
+#pragma unroll
+        for (int k = 0; k < V; ++k) s += k >= at[i].skip ? x[i][k] : 0.f;
+      }
+    }
+    // (divided: the product with a rounded 1 / cols would not give a constant row its own value)
+    const float mean = total(s, 0) / cols;
+    float q = 0.f;
+#pragma unroll
+    for (int i = 0; i < K; ++i) {
+      if (whole<S>(i, a.cols)) {
+#pragma unroll
+        for (int k = 0; k < V; ++k) q = fmaf(x[i][k] - mean, x[i][k] - mean, q);
+      } else {
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+          const float d = k >= at[i].skip ? x[i][k] - mean : 0.f;
+          q = fmaf(d, d, q);
+        }
+      }
+    }
+    const float r = 1.f / sqrtf(total(q, 1) / cols + a.eps);
+    if (!row) continue;
+    if (pos == 0) {
+      if (a.mean) a.mean[n] = mean;
+      if (a.rstd) a.rstd[n] = r;
+    }
+#pragma unroll
+    for (int i = 0; i < K; ++i) {
+      float o[V];
+#pragma unroll
+      for (int k = 0; k < V; ++k) o[k] = fmaf((x[i][k] - mean) * r, w[i][k], b[i][k]);
+      st_window(static_cast<T*>(a.y) + n * a.ldy, at[i], o);
+    }
   }
 }
 
 hipError_t launch_norm(int bf16, const NormArgs& a, hipStream_t s) {
-  // 2^32 threads in x are not launched: beyond 2^22 workgroups they run on over y
   auto run = [&](auto sh) {
-    const int64_t n = (a.rows + sh.groups - 1) / sh.groups, x = std::min<int64_t>(n, 1 << 22);
-    return launch1(ops_norm<decltype(sh)>, x, sh.threads, a, s, (uint32_t)((n + x - 1) / x));
+    const int64_t n = (a.rows + sh.groups - 1) / sh.groups;
+    return launch1(ops_norm<decltype(sh)>, std::min<int64_t>(n, kNormGroups), sh.threads, a, s);
   };
-  return bf16 ? with_row_shape<uint16_t>(a.cols, run) : with_row_shape<float>(a.cols, run);
+  return bf16 ? with_norm_shape<uint16_t>(a.cols, run) : with_norm_shape<float>(a.cols, run);
 }
 
 namespace {
@@ -409,19 +540,14 @@ namespace {
 // A workgroup's sums of its rows' columns into `part` (NULL: not wanted), its
 // row groups added in order in LDS.
 template <typename S, typename A>
-__device__ __forceinline__ void st_norm_part(const A& acc, float* comb, int grp, int pos, int cols, float* part) {
+__device__ __forceinline__ void st_norm_part(const A& acc, const Window* at, float* comb, int grp, int cols, float* part) {
   constexpr int V = Chunk<typename S::T>::V;
   if (!part) return;
 #pragma unroll
   for (int i = 0; i < S::K; ++i)
 #pragma unroll
-    for (int k = 0; k < V; ++k) {
-      const int c = (pos + i * S::lanes) * V + k;
-      if constexpr (S::bwd_groups > 1)
-        comb[grp * S::cols + c] = acc[i][k];
-      else if (c < cols)
-        part[c] = acc[i][k];
-    }
+    for (int k = 0; k < V; ++k)
+      if (k >= at[i].skip) (S::bwd_groups > 1 ? comb + grp * S::cols : part)[at[i].at + k] = acc[i][k];
   if constexpr (S::bwd_groups > 1) {
     __syncthreads();
     for (int c = threadIdx.x; c < cols; c += 1024) {
@@ -439,10 +565,11 @@ __device__ __forceinline__ void st_norm_part(const A& acc, float* comb, int grp,
 // db in registers over all its rows.  At the end the workgroup's row groups are
 // added in order through LDS and one partial row per workgroup is stored (a
 // single workgroup stores dw and db themselves).  Workgroups of 1024 threads, one
-// a compute unit, keep the partial rows few: 16384 x 512 bf16 with res takes 18.7
-// us with 256 of them, 23.3 with 512 of 256 threads, 31 with 256 of 256 (too few
-// rows in flight).  The next row's loads ahead of the reduction gain nothing over
-// the other waves' (18.8).
+// a compute unit, keep the partial rows few: 16384 x 512 bf16 with res takes 19.7
+// us with 256 of them (4 of it the launch that adds them up), 23 with 512 of 256
+// threads, 31 with 256 of 256 (too few rows in flight).  16384 x 4096 takes 86.7
+// us, 4.6 TB/s.  The next row's loads ahead of the reduction gain nothing over the
+// other waves'.
 template <typename S>
 __global__ __launch_bounds__(1024) void ops_norm_bwd(NormBwdArgs a) {
   typedef typename S::T T;
@@ -451,10 +578,11 @@ __global__ __launch_bounds__(1024) void ops_norm_bwd(NormBwdArgs a) {
   __shared__ float comb[G > 1 ? G * S::cols : 1];
   const int grp = threadIdx.x / S::lanes, pos = threadIdx.x % S::lanes;
   float w[K][V], aw[K][V], ab[K][V];
+  Window at[K];
 #pragma unroll
   for (int i = 0; i < K; ++i) {
-    const int c = (pos + i * S::lanes) * V;
-    ld_vector<V>(a.w, c, a.cols - c, 1.f, w[i]);
+    at[i] = window<S>(pos, i, a.cols);
+    ld_weights<S>(a.w, at[i], 1.f, w[i]);
 #pragma unroll
     for (int k = 0; k < V; ++k) aw[i][k] = ab[i][k] = 0.f;
   }
@@ -462,15 +590,25 @@ __global__ __launch_bounds__(1024) void ops_norm_bwd(NormBwdArgs a) {
   int buf = 0;
   // the same number of rounds for every row group of the workgroup
   for (int64_t n0 = (int64_t)blockIdx.x * G; n0 < a.rows; n0 += (int64_t)gridDim.x * G) {
-    const int64_t n = n0 + grp;
-    const bool row = n < a.rows;  // behind the last row: zeros, which add nothing
-    const float mean = row ? a.mean[n] : 0.f, r = row ? a.rstd[n] : 0.f;
+    const bool row = n0 + grp < a.rows;
+    const int64_t n = row ? n0 + grp : n0;  // (behind the last row: an existing one)
+    const float mean = a.mean[n], r = a.rstd[n];
     Chunk<T> x[K], d[K];
 #pragma unroll
     for (int i = 0; i < K; ++i) {
-      const int c = (pos + i * S::lanes) * V, left = row ? a.cols - c : 0;
-      x[i] = ld_chunk(static_cast<const T*>(a.x) + n * a.ldx + c, left);
-      d[i] = ld_chunk(static_cast<const T*>(a.dy) + n * a.lddy + c, left);
+      x[i] = ld_window<S>(static_cast<const T*>(a.x) + n * a.ldx, at[i]);
+      d[i] = ld_window<S>(static_cast<const T*>(a.dy) + n * a.lddy, at[i]);
+    }
+    // what is not the thread's adds nothing: columns of the chunk before, rows behind the last
+#pragma unroll
+    for (int i = 0; i < K; ++i)
+      if (!whole<S>(i, a.cols)) {
+        clear_front(x[i], at[i].skip);
+        clear_front(d[i], at[i].skip);
+      }
+    if (!row) {
+#pragma unroll
+      for (int i = 0; i < K; ++i) d[i].r = u32x4_t{0u, 0u, 0u, 0u};
     }
     float sg = 0.f, sgh = 0.f;
 #pragma unroll
@@ -501,25 +639,23 @@ __global__ __launch_bounds__(1024) void ops_norm_bwd(NormBwdArgs a) {
     const float mg = sg * inv, mgh = sgh * inv;
 #pragma unroll
     for (int i = 0; i < K; ++i) {
-      const int c = (pos + i * S::lanes) * V;
-      if (c >= a.cols) continue;
       // g and h are unpacked again: held over the reduction they cost 2 K V registers
       asm volatile("" : "+v"(x[i].r), "+v"(d[i].r));
       Chunk<T> res;
       res.r = u32x4_t{0u, 0u, 0u, 0u};
-      if (a.res) res = ld_chunk(static_cast<const T*>(a.res) + n * a.ldres + c, a.cols - c);
+      if (a.res) res = ld_window<S>(static_cast<const T*>(a.res) + n * a.ldres, at[i]);
       float o[V];
 #pragma unroll
       for (int k = 0; k < V; ++k) o[k] = fmaf(r, d[i][k] * w[i][k] - mg - (x[i][k] - mean) * r * mgh, res[k]);
-      st_chunk(static_cast<T*>(a.dx) + n * a.lddx + c, a.cols - c, o);
+      st_window(static_cast<T*>(a.dx) + n * a.lddx, at[i], o);
     }
   }
   if (!a.part) return;
   const bool alone = a.nparts == 1;
   float* part = a.part + (int64_t)blockIdx.x * 2 * a.ldpart;
-  st_norm_part<S>(aw, comb, grp, pos, a.cols, alone ? a.dw : part);
+  st_norm_part<S>(aw, at, comb, grp, a.cols, alone ? a.dw : part);
   if constexpr (G > 1) __syncthreads();
-  st_norm_part<S>(ab, comb, grp, pos, a.cols, alone ? a.db : part + a.ldpart);
+  st_norm_part<S>(ab, at, comb, grp, a.cols, alone ? a.db : part + a.ldpart);
 }
 
 // Partial rows: one per workgroup, a workgroup per compute unit; a single one
@@ -529,12 +665,12 @@ int norm_bwd_parts(int bf16, int64_t rows, int cols) {
     constexpr int g = decltype(sh)::bwd_groups;
     return rows <= 2 * g ? 1 : (int)std::min<int64_t>((rows + g - 1) / g, 256);
   };
-  return bf16 ? with_row_shape<uint16_t>(cols, parts) : with_row_shape<float>(cols, parts);
+  return bf16 ? with_norm_bwd_shape<uint16_t>(cols, parts) : with_norm_bwd_shape<float>(cols, parts);
 }
 
 hipError_t launch_norm_bwd(int bf16, const NormBwdArgs& a, hipStream_t s) {
   auto run = [&](auto sh) { return launch1(ops_norm_bwd<decltype(sh)>, a.nparts, 1024, a, s); };
-  return bf16 ? with_row_shape<uint16_t>(a.cols, run) : with_row_shape<float>(a.cols, run);
+  return bf16 ? with_norm_bwd_shape<uint16_t>(a.cols, run) : with_norm_bwd_shape<float>(a.cols, run);
 }
 
 // dw and db from the partial rows ([slice][dw | db][ldpart]): 16 columns a
