@@ -432,7 +432,8 @@ hipError_t launch_norm(int bf16, const NormArgs& a, hipStream_t s);
 // Its backward: dx (nullable) and, over norm_bwd_parts() slices of the rows,
 // partial sums part[slice][0: dw, 1: db][ldpart] (part nullable: no sums
 // wanted), which launch_norm_sum adds in order into dw and db (each nullable).  A
-// single slice goes into dw and db at once.
+// single slice goes into dw and db at once; so do strips of columns where
+// norm_bwd_strips() says that they pay.
 struct NormBwdArgs {
   const void* x; int64_t ldx;
   const void* dy; int64_t lddy;
@@ -441,10 +442,12 @@ struct NormBwdArgs {
   void* dx; int64_t lddx;
   float* part; int64_t ldpart; int nparts;
   float* dw; float* db;
+  int strips;  // dw and db by workgroups of their own, beside dx (which may not be dy then)
   int64_t rows;
   int cols;
 };
 int norm_bwd_parts(int bf16, int64_t rows, int cols);
+bool norm_bwd_strips(int64_t rows);
 inline int64_t norm_part_pitch(int cols) { return (cols + 3) / 4 * 4; }
 hipError_t launch_norm_bwd(int bf16, const NormBwdArgs& a, hipStream_t s);
 hipError_t launch_norm_sum(const float* part, int64_t ldpart, int nparts, int cols, float* dw, float* db, hipStream_t s);

@@ -559,6 +559,66 @@ __device__ __forceinline__ void st_norm_part(const A& acc, const Window* at, flo
   }
 }
 
+// A thread's part of x and dy of row n, and the row's statistics.
+template <typename S>
+struct NormRow {
+  Chunk<typename S::T> x[S::K], d[S::K];
+  float mean, r;
+};
+template <typename S>
+__device__ __forceinline__ NormRow<S> ld_norm_row(const NormBwdArgs& a, const Window* at, int64_t n) {
+  typedef typename S::T T;
+  NormRow<S> v;
+  v.mean = a.mean[n];
+  v.r = a.rstd[n];
+#pragma unroll
+  for (int i = 0; i < S::K; ++i) {
+    v.x[i] = ld_window<S>(static_cast<const T*>(a.x) + n * a.ldx, at[i]);
+    v.d[i] = ld_window<S>(static_cast<const T*>(a.dy) + n * a.lddy, at[i]);
+  }
+  return v;
+}
+
+// dw and db of 16 chunks of columns over all rows, 64 rows at a time: with few
+// rows these workgroups run beside those of dx (which has its row sums from the
+// forward's statistics either way), and no launch adds partial rows up.
+template <typename S>
+__device__ __forceinline__ void norm_strip(const NormBwdArgs& a, int strip, float* comb) {
+  typedef typename S::T T;
+  constexpr int V = Chunk<T>::V;
+  typedef RowShape<T, 16, 1, 1, S::narrow> C;
+  const int grp = threadIdx.x >> 4, pos = threadIdx.x & 15;
+  const Window at = window<C>(strip * 16 + pos, 0, a.cols);
+  float aw[V] = {}, ab[V] = {};
+#pragma unroll 4
+  for (int64_t n = grp; n < a.rows; n += 64) {
+    const NormRow<C> v = ld_norm_row<C>(a, &at, n);
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+      aw[k] = fmaf(v.d[0][k], (v.x[0][k] - v.mean) * v.r, aw[k]);
+      ab[k] += v.d[0][k];
+    }
+  }
+  const int c0 = strip * 16 * V;
+  for (int which = 0; which < 2; ++which) {
+    float* out = which ? a.db : a.dw;
+    if (!out) continue;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < V; ++k) comb[(grp * 16 + pos) * V + k] = which ? ab[k] : aw[k];
+    __syncthreads();
+    // column c of the strip: the window slot that holds it as its own
+    const int c = c0 + (int)threadIdx.x;
+    if ((int)threadIdx.x < 16 * V && c < a.cols) {
+      const int l = (int)threadIdx.x / V, s = c - window<C>(strip * 16 + l, 0, a.cols).at;
+      float v = 0.f;
+#pragma unroll 8
+      for (int g = 0; g < 64; ++g) v += comb[(g * 16 + l) * V + s];
+      out[c] = v;
+    }
+  }
+}
+
 }  // namespace
 
 // Backward.  A thread keeps its columns' weights and its partial sums of dw and
@@ -568,14 +628,19 @@ __device__ __forceinline__ void st_norm_part(const A& acc, const Window* at, flo
 // a compute unit, keep the partial rows few: 16384 x 512 bf16 with res takes 19.7
 // us with 256 of them (4 of it the launch that adds them up), 23 with 512 of 256
 // threads, 31 with 256 of 256 (too few rows in flight).  16384 x 4096 takes 86.7
-// us, 4.6 TB/s.  The next row's loads ahead of the reduction gain nothing over the
-// other waves'.
+// us, 4.6 TB/s.  The next row's loads are issued ahead where a row's
+// waves meet at a barrier (17495 x 1083: 42.9 us, 47.0 without; rows of one wave
+// lose up to a tenth by it).
 template <typename S>
 __global__ __launch_bounds__(1024) void ops_norm_bwd(NormBwdArgs a) {
   typedef typename S::T T;
   constexpr int V = Chunk<T>::V, G = S::bwd_groups, L = S::L, W = S::W, K = S::K;
   __shared__ float2 sums[2][G][W];
-  __shared__ float comb[G > 1 ? G * S::cols : 1];
+  __shared__ float comb[G > 1 ? G * S::cols : 1024 * V];
+  if ((int)blockIdx.x >= a.nparts) {
+    norm_strip<S>(a, (int)blockIdx.x - a.nparts, comb);
+    return;
+  }
   const int grp = threadIdx.x / S::lanes, pos = threadIdx.x % S::lanes;
   float w[K][V], aw[K][V], ab[K][V];
   Window at[K];
@@ -588,17 +653,22 @@ __global__ __launch_bounds__(1024) void ops_norm_bwd(NormBwdArgs a) {
   }
   const float inv = 1.f / (float)a.cols;
   int buf = 0;
+  const int64_t first = (int64_t)blockIdx.x * G;
+  NormRow<S> cur, next;
+  constexpr bool kAhead = W > 1 && K * V <= 8;
+  if constexpr (kAhead) next = ld_norm_row<S>(a, at, first + grp < a.rows ? first + grp : first);
   // the same number of rounds for every row group of the workgroup
-  for (int64_t n0 = (int64_t)blockIdx.x * G; n0 < a.rows; n0 += (int64_t)gridDim.x * G) {
-    const bool row = n0 + grp < a.rows;
-    const int64_t n = row ? n0 + grp : n0;  // (behind the last row: an existing one)
-    const float mean = a.mean[n], r = a.rstd[n];
-    Chunk<T> x[K], d[K];
-#pragma unroll
-    for (int i = 0; i < K; ++i) {
-      x[i] = ld_window<S>(static_cast<const T*>(a.x) + n * a.ldx, at[i]);
-      d[i] = ld_window<S>(static_cast<const T*>(a.dy) + n * a.lddy, at[i]);
+  for (int64_t n0 = first; n0 < a.rows; n0 += (int64_t)a.nparts * G) {
+    const bool row = n0 + grp < a.rows;  // (behind the last row: an existing one)
+    const int64_t n = row ? n0 + grp : n0, ahead = n0 + (int64_t)a.nparts * G;
+    if constexpr (kAhead) {
+      cur = next;
+      if (ahead < a.rows) next = ld_norm_row<S>(a, at, ahead + grp < a.rows ? ahead + grp : ahead);
+    } else {
+      cur = ld_norm_row<S>(a, at, n);
     }
+    Chunk<T>(&x)[K] = cur.x, (&d)[K] = cur.d;
+    const float mean = cur.mean, r = cur.r;
     // what is not the thread's adds nothing: columns of the chunk before, rows behind the last
 #pragma unroll
     for (int i = 0; i < K; ++i)
@@ -651,7 +721,7 @@ __global__ __launch_bounds__(1024) void ops_norm_bwd(NormBwdArgs a) {
     }
   }
   if (!a.part) return;
-  const bool alone = a.nparts == 1;
+  const bool alone = a.nparts == 1;  // (the whole of dw and db)
   float* part = a.part + (int64_t)blockIdx.x * 2 * a.ldpart;
   st_norm_part<S>(aw, at, comb, grp, a.cols, alone ? a.dw : part);
   if constexpr (G > 1) __syncthreads();
@@ -668,8 +738,23 @@ int norm_bwd_parts(int bf16, int64_t rows, int cols) {
   return bf16 ? with_norm_bwd_shape<uint16_t>(cols, parts) : with_norm_bwd_shape<float>(cols, parts);
 }
 
-hipError_t launch_norm_bwd(int bf16, const NormBwdArgs& a, hipStream_t s) {
-  auto run = [&](auto sh) { return launch1(ops_norm_bwd<decltype(sh)>, a.nparts, 1024, a, s); };
+// Strips read x and dy once more, and take a round for every 64 rows: 270 x 512
+// bf16 in 8.6 us (host time) against 11.3 with two launches, 700 x 8192 16.0 / 26.7;
+// from 1000 rows on no faster (1000 x 2048 13.1 / 11.3).
+bool norm_bwd_strips(int64_t rows) { return rows <= 768; }
+
+hipError_t launch_norm_bwd(int bf16, const NormBwdArgs& args, hipStream_t s) {
+  NormBwdArgs a = args;
+  auto run = [&](auto sh) {
+    typedef decltype(sh) S;
+    const int strip = 16 * Chunk<typename S::T>::V;
+    const int strips = a.strips ? (a.cols + strip - 1) / strip : 0;
+    if (a.strips) {
+      a.part = nullptr;  // the first workgroups give dx alone
+      a.nparts = a.dx ? (int)((a.rows + S::bwd_groups - 1) / S::bwd_groups) : 0;
+    }
+    return launch1(ops_norm_bwd<S>, a.nparts + strips, 1024, a, s);
+  };
   return bf16 ? with_norm_bwd_shape<uint16_t>(a.cols, run) : with_norm_bwd_shape<float>(a.cols, run);
 }
 

@@ -313,6 +313,7 @@ erase_status erase_layer_norm_backward(const erase_norm_config* cfg, const void*
   const int64_t ldp = norm_part_pitch(c.cols);
   float* part = sums ? static_cast<float*>(scratch) : nullptr;
   const int nparts = c.rows > 0 ? norm_bwd_parts(bf16, c.rows, c.cols) : 0;
+  const bool strips = sums && nparts > 1 && dx != dy && norm_bwd_strips(c.rows);
   if (c.rows > 0 && (dx || sums)) {
     NormBwdArgs a{};
     a.x = x;
@@ -329,13 +330,14 @@ erase_status erase_layer_norm_backward(const erase_norm_config* cfg, const void*
     a.part = part;
     a.ldpart = ldp;
     a.nparts = nparts;
+    a.strips = strips;
     a.dw = dw;
     a.db = db;
     a.rows = c.rows;
     a.cols = c.cols;
     if (launch_norm_bwd(bf16, a, s) != hipSuccess) return ERASE_ERR_HIP;
   }
-  return sums && nparts != 1 ? done(launch_norm_sum(part, ldp, nparts, c.cols, dw, db, s)) : ERASE_OK;
+  return sums && nparts != 1 && !strips ? done(launch_norm_sum(part, ldp, nparts, c.cols, dw, db, s)) : ERASE_OK;
 }
 
 erase_status erase_dropout(const erase_dropout_config* cfg, const void* x, const void* res, void* y,

@@ -362,6 +362,14 @@ def test_layer_norm_backward_pitches_and_aliases(dtype, C, lead, gap, alias):
     _norm_bwd_case(dtype, 130, C, lead=lead, gap=gap, alias=None if alias == "res" else alias)
 
 
+@pytest.mark.parametrize("R", [32, 33, 64, 65, 768, 769])
+@pytest.mark.parametrize("dtype,C", [("bf16", 5), ("bf16", 512), ("f32", 515), ("bf16", 1030), ("f32", 3), ("bf16", 5000)])
+def test_layer_norm_backward_around_one_launch(dtype, R, C):
+    """Row counts on both sides of those that one launch serves, also with dx over dy."""
+    _norm_bwd_case(dtype, R, C, gap=1)
+    _norm_bwd_case(dtype, R, C, alias="dy")
+
+
 @pytest.mark.parametrize("need", [(True, False, False), (False, True, False), (False, False, True), (True, True, False),
                                   (False, True, True), (True, False, True), (False, False, False)])
 @pytest.mark.parametrize("R", [0, 7, 600])
