@@ -26,11 +26,20 @@
  * sticky, one context per host thread, no device allocation after init.
  * bf16 GEMM operands and stored activations, fp32 accumulation, fp32 master
  * parameters, moments, gradients, statistics and losses.
+ *
+ * erase_tf_options adds to every block, each on request: rotary positions of the
+ * queries and keys, layer norm with learned weight and bias in the place of each
+ * rms, and dropout of the two branches,
+ *   n1 = ln(a0; g1, b1);  [q | k | v] = n1 Wqkv^T;  q, k turned by position t
+ *   a1 = a0 + drop(o Wo^T);  n2 = ln(a1; g2, b2);  z = a1 + drop(gelu(n2 W1^T) W2^T)
+ *   l_b from ln(z; g3, b3)
+ * with the operators of erase_ops.h.
  */
 #ifndef ERASE_TF_H_
 #define ERASE_TF_H_
 
 #include "erase.h"
+#include "erase_ops.h"
 
 #ifdef __cplusplus
 extern "C" {
@@ -71,6 +80,33 @@ ERASE_API erase_status erase_tf_workspace_bytes(const erase_tf_config* cfg, size
 ERASE_API erase_status erase_tf_init(const erase_tf_config* cfg, const erase_block_buffers* bufs, void* workspace,
                            size_t ws_bytes, void* s_fwd, void* s_bwd, erase_tf_ctx** ctx_out);
 
+/* What the blocks have beside the plain step.  A branch's masks come from
+ * erase_dropout's generator with key `seed`, row = position b T + t, column, and
+ * offset ((2 block + branch) << 40) + the step's number (branch 0: attention, 1:
+ * MLP), so that a resumed run draws the masks of an uninterrupted one. */
+typedef enum { ERASE_TF_NORM_RMS = 0, ERASE_TF_NORM_LAYER = 1 } erase_tf_norm;
+
+typedef struct {
+  int32_t rope;               /* 1: queries and keys are turned, 0: not (the next two are not read) */
+  int32_t rope_layout;        /* erase_rope_layout */
+  erase_rope_spec rope_spec;  /* rot_dim at most 64, the head size */
+  int32_t norm;               /* erase_tf_norm */
+  float norm_eps;             /* of the layer norms: >= 0, finite */
+  double dropout;             /* p of both branches, 0..1; 0: no dropout */
+  uint64_t seed;
+} erase_tf_options;
+
+/* erase_tf_param_count(), erase_tf_workspace_bytes() and erase_tf_init() with
+ * options (NULL: none; the calls without options are these with NULL).  With
+ * layer norms a block's parameters end with g1, b1, g2, b2, g3, b3, [d] each. */
+ERASE_API erase_status erase_tf_param_count_options(const erase_tf_config* cfg, const erase_tf_options* opt,
+                                                    int32_t block, int64_t* count);
+ERASE_API erase_status erase_tf_workspace_bytes_options(const erase_tf_config* cfg, const erase_tf_options* opt,
+                                                        size_t* bytes);
+ERASE_API erase_status erase_tf_init_options(const erase_tf_config* cfg, const erase_tf_options* opt,
+                                             const erase_block_buffers* bufs, void* workspace, size_t ws_bytes,
+                                             void* s_fwd, void* s_bwd, erase_tf_ctx** ctx_out);
+
 /* Enqueue one training step and return without waiting.
  *   tokens: device int32 [batch][seq_len + 1]; position t of row b reads
  *           tokens[b][t] and predicts tokens[b][t + 1].  An id outside
@@ -108,13 +144,16 @@ ERASE_API erase_status erase_tf_refresh_weights(erase_tf_ctx* ctx);
  * 14 attention forward, 15 attention backward (dK, dV and dQ in one launch,
  * layer 0), 16 softmax normaliser of the vocabulary head (layer 0 every row,
  * 1 the recomputation of out-of-range rows), 17 embedding gradient (four
- * launches, bracketed by stream events rather than kernel-stamped ones). */
+ * launches, bracketed by stream events rather than kernel-stamped ones).  With
+ * options, likewise bracketed: 12 and 13 are the layer norms, 18 rotary positions
+ * (layer 0 forward, 1 backward), 19 dropout (layer 0 and 1 the branches forward, 2
+ * and 3 backward); their grid is 0 (not reported). */
 ERASE_API erase_status erase_tf_set_timing(erase_tf_ctx* ctx, int32_t enable);
 ERASE_API erase_status erase_tf_read_timing(erase_tf_ctx* ctx, erase_kernel_time* out, int32_t cap, int32_t* n);
 
 /* Device address and row pitch (elements) of a stored tensor of block
  * `block`, for inspection after erase_tf_sync():
- *   0 a0, 1 n1, 2 qkv [.][3d], 3 o, 4 a1, 5 n2, 6 u [.][4d] (MLP
+ *   0 a0, 1 n1, 2 qkv [.][3d] (q and k turned where they are), 3 o, 4 a1, 5 n2, 6 u [.][4d] (MLP
  *   pre-activation), 7 gelu(u), 8 z, 9 hn, 10 the head's exponentials
  *   e[n][v] = exp(logit - target logit) [.][V] (bf16; after a step the
  *   target entry holds e - S_n, S_n the row's sum, so that rowscale[n] e[n]

@@ -417,7 +417,10 @@ struct RopeFillArgs {
 hipError_t launch_rope_fill(const RopeFillArgs& a, hipStream_t s);
 hipError_t launch_rope(int bf16, const RopeArgs& a, hipStream_t s);
 
-// Layer norm; w, b, mean and rstd as in the C ABI (nullable).
+// Layer norm; w, b, mean and rstd as in the C ABI (nullable).  With hw set (the
+// vocabulary head's bf16 weight [V][ldhw]; bf16 rows of a multiple of 64 columns,
+// 4096 at most) also the target logit xref[n] = y[n] . hw[target[n]] of the stored
+// row (0 where the target is invalid).
 struct NormArgs {
   const void* x; int64_t ldx;
   const float* w; const float* b;
@@ -426,6 +429,9 @@ struct NormArgs {
   int64_t rows;
   int cols;
   float eps;
+  const uint16_t* hw; int64_t ldhw;
+  const int32_t* target;
+  float* xref;
 };
 hipError_t launch_norm(int bf16, const NormArgs& a, hipStream_t s);
 
@@ -445,6 +451,12 @@ struct NormBwdArgs {
   int strips;  // dw and db by workgroups of their own, beside dx (which may not be dy then)
   int64_t rows;
   int cols;
+  // bf16 rows of a multiple of 64 columns, 4096 at most: with dyscale set the
+  // gradient is dyscale[n] dy[n], dy the sum of nslice fp32 slices
+  // slice[z][n][ldslice] where nslice > 0; with dx32 set dx is stored in fp32 there
+  const float* dyscale;
+  const float* slice; int64_t ldslice, zslice; int nslice;
+  float* dx32; int64_t lddx32;
 };
 int norm_bwd_parts(int bf16, int64_t rows, int cols);
 bool norm_bwd_strips(int64_t rows);
@@ -466,5 +478,10 @@ struct DropArgs {
   float scale;
 };
 hipError_t launch_dropout(int bf16, const DropArgs& a, hipStream_t s);
+// `limit` and `scale` of a probability: steps of 2^-16, the scale exact for the step.
+inline void drop_rate(double p, DropArgs* a) {
+  a->limit = uint32_t(p * 65536.0 + 0.5);
+  a->scale = a->limit < 65536 ? float(65536.0 / (65536 - a->limit)) : 0.f;
+}
 
 }  // namespace erase

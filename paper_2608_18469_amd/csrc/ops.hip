@@ -449,11 +449,12 @@ constexpr int kNormGroups = 2048;  // workgroups of the forward, eight a compute
 // rows, so that weight and bias (twice the bytes of a bf16 row each) are read
 // once per thread, not per row: 8000 x 4096 bf16 takes 27.7 us (4.7 TB/s), 34.9
 // with weight and bias read again for every row.
-template <typename S>
+// HEAD: also the target logit of the stored row.
+template <typename S, bool HEAD>
 __global__ __launch_bounds__(S::threads) void ops_norm(NormArgs a) {
   typedef typename S::T T;
   constexpr int V = Chunk<T>::V, L = S::L, W = S::W, K = S::K;
-  __shared__ float sums[2][S::groups][W];
+  __shared__ float sums[HEAD ? 3 : 2][S::groups][W];
   const int grp = threadIdx.x / S::lanes, pos = threadIdx.x % S::lanes;
   const float cols = (float)a.cols;
   float w[K][V], b[K][V];
@@ -512,26 +513,46 @@ __global__ __launch_bounds__(S::threads) void ops_norm(NormArgs a) {
       }
     }
     const float r = 1.f / sqrtf(total(q, 1) / cols + a.eps);
-    if (!row) continue;
-    if (pos == 0) {
+    if (!HEAD && !row) continue;
+    if (row && pos == 0) {
       if (a.mean) a.mean[n] = mean;
       if (a.rstd) a.rstd[n] = r;
     }
+    const int32_t target = HEAD ? a.target[n] : -1;
+    float logit = 0.f;
 #pragma unroll
     for (int i = 0; i < K; ++i) {
       float o[V];
 #pragma unroll
       for (int k = 0; k < V; ++k) o[k] = fmaf((x[i][k] - mean) * r, w[i][k], b[i][k]);
-      st_window(static_cast<T*>(a.y) + n * a.ldy, at[i], o);
+      if (row) st_window(static_cast<T*>(a.y) + n * a.ldy, at[i], o);
+      if constexpr (HEAD) {
+        if (target >= 0) {  // (whole chunks: cols is a multiple of V)
+          const Chunk<T> c = pack_chunk<T>(o), hw = ld_window<S>(a.hw + (int64_t)target * a.ldhw, at[i]);
+#pragma unroll
+          for (int k = 0; k < V; ++k) logit = fmaf(at[i].skip ? 0.f : c[k], hw[k], logit);
+        }
+      }
+    }
+    if constexpr (HEAD) {
+      logit = total(logit, 2);
+      if (row && pos == 0) a.xref[n] = logit;
     }
   }
 }
 
 hipError_t launch_norm(int bf16, const NormArgs& a, hipStream_t s) {
-  auto run = [&](auto sh) {
-    const int64_t n = (a.rows + sh.groups - 1) / sh.groups;
-    return launch1(ops_norm<decltype(sh)>, std::min<int64_t>(n, kNormGroups), sh.threads, a, s);
-  };
+  auto grid = [&](auto sh) { return std::min<int64_t>((a.rows + sh.groups - 1) / sh.groups, kNormGroups); };
+  if (a.hw) {
+    if (!bf16 || a.cols % 64 || a.cols > 4096) return hipErrorInvalidValue;
+    auto run = [&](auto sh) {
+      typedef decltype(sh) S;
+      if constexpr (!S::narrow && S::cols <= 4096) return launch1(ops_norm<S, true>, grid(sh), sh.threads, a, s);
+      return hipErrorInvalidValue;
+    };
+    return with_norm_shape<uint16_t>(a.cols, run);
+  }
+  auto run = [&](auto sh) { return launch1(ops_norm<decltype(sh), false>, grid(sh), sh.threads, a, s); };
   return bf16 ? with_norm_shape<uint16_t>(a.cols, run) : with_norm_shape<float>(a.cols, run);
 }
 
@@ -559,22 +580,63 @@ __device__ __forceinline__ void st_norm_part(const A& acc, const Window* at, flo
   }
 }
 
+// What the backward takes and gives: PLAIN is the public operator; HEAD takes a
+// row scale and, where there are slices, their sum as dy; F32 stores dx in fp32.
+enum NormMode { PLAIN, HEAD, F32 };
+
+// Elements in fp32 with a Chunk's reading.
+template <int V>
+struct Floats {
+  float v[V];
+  __device__ __forceinline__ float operator[](int k) const { return v[k]; }
+};
+template <int V>
+__device__ __forceinline__ void clear_front(Floats<V>& c, int skip) {
+#pragma unroll
+  for (int k = 0; k < V; ++k) c.v[k] = k >= skip ? c.v[k] : 0.f;
+}
+
 // A thread's part of x and dy of row n, and the row's statistics.
-template <typename S>
+template <typename S, NormMode M>
 struct NormRow {
-  Chunk<typename S::T> x[S::K], d[S::K];
+  typedef Chunk<typename S::T> C;
+  C x[S::K];
+  std::conditional_t<M == HEAD, Floats<C::V>, C> d[S::K];
   float mean, r;
 };
-template <typename S>
-__device__ __forceinline__ NormRow<S> ld_norm_row(const NormBwdArgs& a, const Window* at, int64_t n) {
+template <typename S, NormMode M>
+__device__ __forceinline__ NormRow<S, M> ld_norm_row(const NormBwdArgs& a, const Window* at, int64_t n) {
   typedef typename S::T T;
-  NormRow<S> v;
+  constexpr int V = Chunk<T>::V;
+  NormRow<S, M> v;
   v.mean = a.mean[n];
   v.r = a.rstd[n];
 #pragma unroll
   for (int i = 0; i < S::K; ++i) {
     v.x[i] = ld_window<S>(static_cast<const T*>(a.x) + n * a.ldx, at[i]);
-    v.d[i] = ld_window<S>(static_cast<const T*>(a.dy) + n * a.lddy, at[i]);
+    if constexpr (M == HEAD) {
+      float(&d)[V] = v.d[i].v;
+      if (a.nslice > 0) {
+#pragma unroll
+        for (int k = 0; k < V; ++k) d[k] = 0.f;
+        const float* p = a.slice + n * a.ldslice + at[i].at;
+        for (int z = 0; z < a.nslice; ++z, p += a.zslice)  // added in order
+#pragma unroll
+          for (int j = 0; j < V; j += 4) {
+            const float4 t = *reinterpret_cast<const float4*>(p + j);
+            d[j] += t.x, d[j + 1] += t.y, d[j + 2] += t.z, d[j + 3] += t.w;
+          }
+      } else {
+        const Chunk<T> c = ld_window<S>(static_cast<const T*>(a.dy) + n * a.lddy, at[i]);
+#pragma unroll
+        for (int k = 0; k < V; ++k) d[k] = c[k];
+      }
+      const float scale = a.dyscale[n];
+#pragma unroll
+      for (int k = 0; k < V; ++k) d[k] *= scale;
+    } else {
+      v.d[i] = ld_window<S>(static_cast<const T*>(a.dy) + n * a.lddy, at[i]);
+    }
   }
   return v;
 }
@@ -592,7 +654,7 @@ __device__ __forceinline__ void norm_strip(const NormBwdArgs& a, int strip, floa
   float aw[V] = {}, ab[V] = {};
 #pragma unroll 4
   for (int64_t n = grp; n < a.rows; n += 64) {
-    const NormRow<C> v = ld_norm_row<C>(a, &at, n);
+    const NormRow<C, PLAIN> v = ld_norm_row<C, PLAIN>(a, &at, n);
 #pragma unroll
     for (int k = 0; k < V; ++k) {
       aw[k] = fmaf(v.d[0][k], (v.x[0][k] - v.mean) * v.r, aw[k]);
@@ -631,16 +693,17 @@ __device__ __forceinline__ void norm_strip(const NormBwdArgs& a, int strip, floa
 // us, 4.6 TB/s.  The next row's loads are issued ahead where a row's
 // waves meet at a barrier (17495 x 1083: 42.9 us, 47.0 without; rows of one wave
 // lose up to a tenth by it).
-template <typename S>
+template <typename S, NormMode M>
 __global__ __launch_bounds__(1024) void ops_norm_bwd(NormBwdArgs a) {
   typedef typename S::T T;
   constexpr int V = Chunk<T>::V, G = S::bwd_groups, L = S::L, W = S::W, K = S::K;
   __shared__ float2 sums[2][G][W];
-  __shared__ float comb[G > 1 ? G * S::cols : 1024 * V];
-  if ((int)blockIdx.x >= a.nparts) {
-    norm_strip<S>(a, (int)blockIdx.x - a.nparts, comb);
-    return;
-  }
+  __shared__ float comb[G > 1 ? G * S::cols : M == PLAIN ? 1024 * V : 1];
+  if constexpr (M == PLAIN)
+    if ((int)blockIdx.x >= a.nparts) {
+      norm_strip<S>(a, (int)blockIdx.x - a.nparts, comb);
+      return;
+    }
   const int grp = threadIdx.x / S::lanes, pos = threadIdx.x % S::lanes;
   float w[K][V], aw[K][V], ab[K][V];
   Window at[K];
@@ -654,20 +717,21 @@ __global__ __launch_bounds__(1024) void ops_norm_bwd(NormBwdArgs a) {
   const float inv = 1.f / (float)a.cols;
   int buf = 0;
   const int64_t first = (int64_t)blockIdx.x * G;
-  NormRow<S> cur, next;
-  constexpr bool kAhead = W > 1 && K * V <= 8;
-  if constexpr (kAhead) next = ld_norm_row<S>(a, at, first + grp < a.rows ? first + grp : first);
+  NormRow<S, M> cur, next;
+  constexpr bool kFew = K * V <= 8, kAhead = W > 1 && kFew;  // elements a thread holds
+  if constexpr (kAhead) next = ld_norm_row<S, M>(a, at, first + grp < a.rows ? first + grp : first);
   // the same number of rounds for every row group of the workgroup
   for (int64_t n0 = first; n0 < a.rows; n0 += (int64_t)a.nparts * G) {
     const bool row = n0 + grp < a.rows;  // (behind the last row: an existing one)
     const int64_t n = row ? n0 + grp : n0, ahead = n0 + (int64_t)a.nparts * G;
     if constexpr (kAhead) {
       cur = next;
-      if (ahead < a.rows) next = ld_norm_row<S>(a, at, ahead + grp < a.rows ? ahead + grp : ahead);
+      if (ahead < a.rows) next = ld_norm_row<S, M>(a, at, ahead + grp < a.rows ? ahead + grp : ahead);
     } else {
-      cur = ld_norm_row<S>(a, at, n);
+      cur = ld_norm_row<S, M>(a, at, n);
     }
-    Chunk<T>(&x)[K] = cur.x, (&d)[K] = cur.d;
+    auto &x = cur.x;
+    auto &d = cur.d;
     const float mean = cur.mean, r = cur.r;
     // what is not the thread's adds nothing: columns of the chunk before, rows behind the last
 #pragma unroll
@@ -678,7 +742,7 @@ __global__ __launch_bounds__(1024) void ops_norm_bwd(NormBwdArgs a) {
       }
     if (!row) {
 #pragma unroll
-      for (int i = 0; i < K; ++i) d[i].r = u32x4_t{0u, 0u, 0u, 0u};
+      for (int i = 0; i < K; ++i) clear_front(d[i], V);
     }
     float sg = 0.f, sgh = 0.f;
 #pragma unroll
@@ -691,7 +755,13 @@ __global__ __launch_bounds__(1024) void ops_norm_bwd(NormBwdArgs a) {
         aw[i][k] = fmaf(dv, h, aw[i][k]);
         ab[i][k] += dv;
       }
-    if (!a.dx) continue;
+    if (M == F32 ? !a.dx32 : !a.dx) continue;
+    Chunk<T> res[K];  // asked for before the sums are known, where registers allow
+#pragma unroll
+    for (int i = 0; i < K; ++i) {
+      res[i].r = u32x4_t{0u, 0u, 0u, 0u};
+      if (kFew && a.res) res[i] = ld_window<S>(static_cast<const T*>(a.res) + n * a.ldres, at[i]);
+    }
     sg = lane_sum<L>(sg);
     sgh = lane_sum<L>(sgh);
     if constexpr (W > 1) {
@@ -710,14 +780,20 @@ __global__ __launch_bounds__(1024) void ops_norm_bwd(NormBwdArgs a) {
 #pragma unroll
     for (int i = 0; i < K; ++i) {
       // g and h are unpacked again: held over the reduction they cost 2 K V registers
-      asm volatile("" : "+v"(x[i].r), "+v"(d[i].r));
-      Chunk<T> res;
-      res.r = u32x4_t{0u, 0u, 0u, 0u};
-      if (a.res) res = ld_window<S>(static_cast<const T*>(a.res) + n * a.ldres, at[i]);
+      asm volatile("" : "+v"(x[i].r));
+      if constexpr (M != HEAD) asm volatile("" : "+v"(d[i].r));
+      if (!kFew && a.res) res[i] = ld_window<S>(static_cast<const T*>(a.res) + n * a.ldres, at[i]);
       float o[V];
 #pragma unroll
-      for (int k = 0; k < V; ++k) o[k] = fmaf(r, d[i][k] * w[i][k] - mg - (x[i][k] - mean) * r * mgh, res[k]);
-      st_window(static_cast<T*>(a.dx) + n * a.lddx, at[i], o);
+      for (int k = 0; k < V; ++k) o[k] = fmaf(r, d[i][k] * w[i][k] - mg - (x[i][k] - mean) * r * mgh, res[i][k]);
+      if constexpr (M == F32) {
+        float* p = a.dx32 + n * a.lddx32 + at[i].at;
+        if (at[i].skip == 0)  // (whole chunks: cols is a multiple of V)
+#pragma unroll
+          for (int k = 0; k < V; k += 4) *reinterpret_cast<float4*>(p + k) = make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
+      } else {
+        st_window(static_cast<T*>(a.dx) + n * a.lddx, at[i], o);
+      }
     }
   }
   if (!a.part) return;
@@ -745,6 +821,16 @@ bool norm_bwd_strips(int64_t rows) { return rows <= 768; }
 
 hipError_t launch_norm_bwd(int bf16, const NormBwdArgs& args, hipStream_t s) {
   NormBwdArgs a = args;
+  if (a.dyscale || a.dx32) {
+    if (!bf16 || a.cols % 64 || a.cols > 4096 || a.strips) return hipErrorInvalidValue;
+    auto run = [&](auto sh) {
+      typedef decltype(sh) S;
+      if constexpr (!S::narrow && S::cols <= 4096)
+        return launch1(a.dyscale ? ops_norm_bwd<S, HEAD> : ops_norm_bwd<S, F32>, a.nparts, 1024, a, s);
+      return hipErrorInvalidValue;
+    };
+    return with_norm_bwd_shape<uint16_t>(a.cols, run);
+  }
   auto run = [&](auto sh) {
     typedef decltype(sh) S;
     const int strip = 16 * Chunk<typename S::T>::V;
@@ -753,7 +839,7 @@ hipError_t launch_norm_bwd(int bf16, const NormBwdArgs& args, hipStream_t s) {
       a.part = nullptr;  // the first workgroups give dx alone
       a.nparts = a.dx ? (int)((a.rows + S::bwd_groups - 1) / S::bwd_groups) : 0;
     }
-    return launch1(ops_norm_bwd<S>, a.nparts + strips, 1024, a, s);
+    return launch1(ops_norm_bwd<S, PLAIN>, a.nparts + strips, 1024, a, s);
   };
   return bf16 ? with_norm_bwd_shape<uint16_t>(a.cols, run) : with_norm_bwd_shape<float>(a.cols, run);
 }

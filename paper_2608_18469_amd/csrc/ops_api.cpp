@@ -195,8 +195,7 @@ erase_status dropout(const erase_dropout_config* cfg, const void* x, const void*
   a.seed = c.seed;
   a.offset = c.offset;
   a.step = step;
-  a.limit = (uint32_t)std::floor(c.p * 65536.0 + 0.5);
-  a.scale = a.limit < 65536 ? (float)(65536.0 / (65536 - a.limit)) : 0.f;
+  drop_rate(c.p, &a);
   return done(launch_dropout(c.dtype == ERASE_BF16, a, static_cast<hipStream_t>(stream)));
 }
 

@@ -83,9 +83,38 @@ erase_status validate(const erase_tf_config* c, std::string* err) {
   return ERASE_OK;
 }
 
-int64_t param_count(const Dims& D, int b) {
+// What a step has beside the plain one.
+struct Opts {
+  bool rope = false, layer = false, drop = false;
+  erase_tf_options o{};
+};
+
+erase_status validate_options(const erase_tf_options* o, Opts* out) {
+  if (!o) return ERASE_OK;
+  if ((o->rope != 0 && o->rope != 1) || (o->norm != ERASE_TF_NORM_RMS && o->norm != ERASE_TF_NORM_LAYER) ||
+      !(o->dropout >= 0 && o->dropout <= 1))
+    return ERASE_ERR_INVALID_ARG;
+  if (o->rope) {
+    if (o->rope_layout < ERASE_ROPE_HALF || o->rope_layout > ERASE_ROPE_INTERLEAVED) return ERASE_ERR_INVALID_ARG;
+    size_t bytes = 0;
+    if (erase_status st = erase_rope_table_bytes(&o->rope_spec, &bytes); st != ERASE_OK) return st;
+    if (o->rope_spec.rot_dim > 64) return ERASE_ERR_SHAPE;
+  }
+  if (o->norm == ERASE_TF_NORM_LAYER && (!(o->norm_eps >= 0) || !std::isfinite(o->norm_eps)))
+    return ERASE_ERR_INVALID_ARG;
+  out->rope = o->rope != 0;
+  out->layer = o->norm == ERASE_TF_NORM_LAYER;
+  out->drop = o->dropout > 0;
+  out->o = *o;
+  return ERASE_OK;
+}
+
+constexpr int kNorms = 3;  // before attention, before the MLP, before the head
+
+int64_t param_count(const Dims& D, const Opts& O, int b) {
   int64_t n = b == 0 ? int64_t(D.V) * D.d : 0;
   for (int i = 0; i < NW; ++i) n += D.rows[i] * D.cols[i];
+  if (O.layer) n += 2 * kNorms * int64_t(D.d);
   return n;
 }
 
@@ -166,6 +195,11 @@ struct Block {
   uint16_t *a0 = nullptr, *n1, *qkv, *o, *a1, *n2, *u, *g, *z, *hn, *logits, *hns;
   uint16_t *dhn = nullptr, *dz, *du, *dn2, *da1, *dout, *dqkv, *dn1 = nullptr;
   float *r1, *r2, *r3, *lse, *lstat, *xref, *rowscale, *rowloss, *ploss, *da0 = nullptr, *gemb = nullptr;
+  // layer norms: offsets of g and b, means (r1..r3 hold 1 / deviation), partial
+  // rows of their gradients
+  int64_t offg[kNorms] = {};
+  float* mean[kNorms] = {};
+  float* npart[kNorms] = {};
   float* dhnp = nullptr;  // the head's input gradient in hsplit fp32 slices [N][d] (hsplit > 1, else dhn)
   int hsplit = 1;
   int32_t* flag = nullptr;
@@ -187,13 +221,21 @@ struct Layout {
   float* hyper = nullptr;
   int32_t *target = nullptr, *input = nullptr, *count = nullptr, *start = nullptr, *fill = nullptr, *cursor = nullptr,
           *bucket = nullptr;
+  Opts O;
+  uint64_t* rope = nullptr;        // table of the rotary positions
+  uint16_t* branch = nullptr;      // a branch's output before its dropout (forward stream)
+  uint16_t* dbranch = nullptr;     // its gradient (backward stream)
+  uint16_t* dn1 = nullptr;         // layer norm: gradient at n1 of the blocks after the first
+  int nparts = 0;                  // partial rows of a layer norm's gradients
+  int64_t ldnp = 0;
   std::vector<Block> blk;
   size_t bytes = 0;
 };
 
-size_t build_layout(const erase_tf_config& c, uintptr_t base, Layout* P) {
+size_t build_layout(const erase_tf_config& c, const Opts& O, uintptr_t base, Layout* P) {
   Dims D = dims_of(c);
   P->D = D;
+  P->O = O;
   Carver cv{base};
   P->t = reinterpret_cast<int64_t*>(base);
   P->status = reinterpret_cast<int*>(base + 8);
@@ -235,6 +277,8 @@ size_t build_layout(const erase_tf_config& c, uintptr_t base, Layout* P) {
       B.sh[i] = bf(rup(D.rows[i], 128), D.cols[i]);
       B.sht[i] = bf(rup(D.cols[i], 128), D.rows[i]);
     }
+    if (O.layer)
+      for (int i = 0; i < kNorms; ++i, off += 2 * d) B.offg[i] = off;
     B.n1 = bf(Np, P->ldd);
     B.qkv = bf(Np, P->ld3);
     B.o = bf(Np, P->ldd);
@@ -271,7 +315,7 @@ size_t build_layout(const erase_tf_config& c, uintptr_t base, Layout* P) {
       // (the MLP-up and attention projections, the vocabulary head), or the
       // weight gradient alone
       WidePair wp;
-      if (i == W1 || i == WO || (i == WQKV && b == 0)) {
+      if (i == W1 || i == WO || (i == WQKV && (b == 0 || O.layer))) {
         wp = wide_pair(D.N, D.rows[i], D.cols[i], 1);
       } else if (i != WH) {
         wp = wide_wgrad(D.rows[i], D.cols[i], D.N, wide_core_wgrad_us(D.rows[i], D.cols[i], D.N, 1), 1);
@@ -289,8 +333,22 @@ size_t build_layout(const erase_tf_config& c, uintptr_t base, Layout* P) {
       else
         B.dhn = bf(Np, P->ldd);
     }
-    B.segs_dev = static_cast<AdamSeg*>(cv.take(sizeof(AdamSeg) * (NW + 1)));
+    B.segs_dev = static_cast<AdamSeg*>(cv.take(sizeof(AdamSeg) * (NW + 1 + (O.layer ? 2 * kNorms : 0))));
+    if (O.layer) {
+      P->nparts = norm_bwd_parts(1, D.N, D.d);
+      P->ldnp = norm_part_pitch(D.d);
+      for (int i = 0; i < kNorms; ++i) {
+        B.mean[i] = f32(Np);
+        B.npart[i] = f32(2 * P->nparts * P->ldnp);
+      }
+    }
   }
+  if (O.rope) P->rope = static_cast<uint64_t*>(cv.take(8 * (size_t(O.o.rope_spec.rot_dim) / 2 + 1)));
+  if (O.drop) {
+    P->branch = bf(Np, P->ldd);
+    P->dbranch = bf(Np, P->ldd);
+  }
+  if (O.layer && D.L > 1) P->dn1 = bf(Np, P->ldd);
   P->bytes = cv.off;
   return cv.off;
 }
@@ -331,14 +389,16 @@ void build_gemms(const erase_tf_config& c, Layout* P) {
       L.e.ldy = ldy;
     };
     fwd(WQKV, B.n1, P->ldd, GK_FWD_LIN, B.qkv, P->ld3);
-    fwd(WO, B.o, P->ldd, GK_FWD_LIN, B.a1, P->ldd);
-    B.fwd[WO].e.res = B.a0;
+    // (with dropout the residual joins behind it)
+    const bool drop = P->O.drop;
+    fwd(WO, B.o, P->ldd, GK_FWD_LIN, drop ? P->branch : B.a1, P->ldd);
+    B.fwd[WO].e.res = drop ? nullptr : B.a0;
     B.fwd[WO].e.ldres = P->ldd;
     fwd(W1, B.n2, P->ldd, GK_FWD_GELU, B.g, P->ld4);
     B.fwd[W1].e.gout = B.u;
     B.fwd[W1].e.ldgout = P->ld4;
-    fwd(W2, B.g, P->ld4, GK_FWD_LIN, B.z, P->ldd);
-    B.fwd[W2].e.res = B.a1;
+    fwd(W2, B.g, P->ld4, GK_FWD_LIN, drop ? P->branch : B.z, P->ldd);
+    B.fwd[W2].e.res = drop ? nullptr : B.a1;
     B.fwd[W2].e.ldres = P->ldd;
     fwd(WH, B.hn, P->ldd, GK_FWD_LOGITS, B.logits, P->ldv);
     // GEMM-core tiles (64 x 128): groups of 8 M-tiles (512 positions), each
@@ -377,12 +437,14 @@ void build_gemms(const erase_tf_config& c, Layout* P) {
       L.e.ldp = d;
       L.e.pstride = N * d;
     }
-    dgr(W2, B.dz, P->ldd, GK_DGRAD_GELU, B.du, P->ld4);
+    const uint16_t *gz = drop ? P->dbranch : B.dz, *ga1 = drop ? P->dbranch : B.da1;  // gradients at the branches' outputs
+    dgr(W2, gz, P->ldd, GK_DGRAD_GELU, B.du, P->ld4);
     B.dgr[W2].e.mask = B.u;
     B.dgr[W2].e.ldmask = P->ld4;
     dgr(W1, B.du, P->ld4, GK_DGRAD, B.dn2, P->ldd);
-    dgr(WO, B.da1, P->ldd, GK_DGRAD, B.dout, P->ldd);
-    if (b == 0) dgr(WQKV, B.dqkv, P->ld3, GK_DGRAD, B.dn1, P->ldd);
+    dgr(WO, ga1, P->ldd, GK_DGRAD, B.dout, P->ldd);
+    // (a layer norm's weights take the gradient at n1 in every block)
+    if (b == 0 || P->O.layer) dgr(WQKV, B.dqkv, P->ld3, GK_DGRAD, b == 0 ? B.dn1 : P->dn1, P->ldd);
 
     // weight gradients: k-major A = output gradient [N][rows], B = layer input [N][cols]
     auto wgr = [&](int w, const void* A, int64_t lda, const void* X, int64_t ldx) {
@@ -395,9 +457,9 @@ void build_gemms(const erase_tf_config& c, Layout* P) {
       L.e.pstride = D.rows[w] * D.cols[w];
     };
     wgr(WH, B.logits, P->ldv, B.hns, P->ldd);  // hns: the row-scaled head input
-    wgr(W2, B.dz, P->ldd, B.g, P->ld4);
+    wgr(W2, gz, P->ldd, B.g, P->ld4);
     wgr(W1, B.du, P->ld4, B.n2, P->ldd);
-    wgr(WO, B.da1, P->ldd, B.o, P->ldd);
+    wgr(WO, ga1, P->ldd, B.o, P->ldd);
     wgr(WQKV, B.dqkv, P->ld3, B.n1, P->ldd);
     // both gradient GEMMs of a weight read the same output gradient: one
     // launch, in the weight gradient's tiles (the plain input-gradient
@@ -435,14 +497,20 @@ void build_segments(Layout* P, const erase_block_buffers* bufs) {
       s.ldsh = cols;
       s.sht = sht;
       s.ldsht = rows;
-      s.vtc = ADAM_TC;
-      s.tcols = (int)cdv(cols, ADAM_TC);
+      s.vtc = rows == 1 ? adam_vtc(nsplit) : ADAM_TC;
+      s.tcols = (int)cdv(cols, s.vtc);
       s.chunk0 = chunk;
       chunk += cdv(rows, ADAM_TR) * s.tcols;
       B.segs.push_back(s);
     };
     if (b == 0) add(0, D.V, D.d, B.gemb, 1, B.cemb, nullptr);
     for (int i = 0; i < NW; ++i) add(B.offw[i], D.rows[i], D.cols[i], B.part[i], B.wp[i].split, B.sh[i], B.sht[i]);
+    if (P->O.layer)
+      for (int i = 0; i < kNorms; ++i)
+        for (int j = 0; j < 2; ++j) {  // g, b: a vector's partials stand 2 ldnp apart
+          add(B.offg[i] + j * D.d, 1, D.d, B.npart[i] + j * P->ldnp, P->nparts, nullptr, nullptr);
+          B.segs.back().pstride = 2 * P->ldnp;
+        }
     B.nchunks = chunk;
   }
 }
@@ -555,6 +623,120 @@ TfRmsArgs rms_args(const Layout& P, const uint16_t* x, float* r, uint16_t* y) {
   return a;
 }
 
+// The layer norm `which` of block b in the place of the rms of `a` (and of the
+// fields that both read): forward, and backward with the partial rows of its
+// weight's and bias's gradients (no dx where nothing takes it).
+erase_status layer_norm(TfCtx* c, const TfRmsArgs& a, int b, int which, int sid, hipStream_t s) {
+  const Layout& P = c->P;
+  const Block& B = P.blk[b];
+  const float* g = B.buf.param + B.offg[which];
+  NormArgs n{};
+  n.x = a.x;
+  n.ldx = a.ldx;
+  n.w = g;
+  n.b = g + P.D.d;
+  n.y = a.y;
+  n.ldy = a.ldy;
+  n.mean = B.mean[which];
+  n.rstd = a.r;
+  n.rows = a.N;
+  n.cols = a.d;
+  n.eps = P.O.o.norm_eps;
+  n.hw = a.hw;
+  n.ldhw = a.ldhw;
+  n.target = a.target;
+  n.xref = a.xref;
+  TFRUN(c, 12, b, which, sid, 0.0, double(a.N) * a.d * 4, 0, [&](const LaunchEv&) { return launch_norm(1, n, s); }, 0, 0, 0,
+        false, s);
+  return ERASE_OK;
+}
+erase_status layer_norm_backward(TfCtx* c, const TfRmsArgs& a, int b, int which, int sid, hipStream_t s) {
+  const Layout& P = c->P;
+  const Block& B = P.blk[b];
+  NormBwdArgs n{};
+  n.x = a.x;
+  n.ldx = a.ldx;
+  n.dy = a.dy;
+  n.lddy = a.lddy;
+  n.w = B.buf.param + B.offg[which];
+  n.mean = B.mean[which];
+  n.rstd = a.r;
+  n.res = a.res;
+  n.ldres = a.ldres;
+  n.dx = a.y;
+  n.lddx = a.ldy;
+  n.dx32 = a.out_f32;
+  n.lddx32 = a.ldout;
+  n.part = B.npart[which];
+  n.ldpart = P.ldnp;
+  n.nparts = P.nparts;
+  n.dw = n.part;
+  n.db = n.part + P.ldnp;
+  n.rows = a.N;
+  n.cols = a.d;
+  n.dyscale = a.dyscale;
+  n.slice = a.dypart;
+  n.ldslice = a.ldpart;
+  n.zslice = a.ppstride;
+  n.nslice = a.npart;
+  TFRUN(c, 13, b, which, sid, 0.0, double(a.N) * a.d * 6, 0, [&](const LaunchEv&) { return launch_norm_bwd(1, n, s); }, 0, 0, 0,
+        false, s);
+  return ERASE_OK;
+}
+
+// The norm before a sub-block, forward or backward, as the options say.
+erase_status norm(TfCtx* c, int backward, const TfRmsArgs& a, int b, int which, int sid, hipStream_t s) {
+  if (!c->P.O.layer) return rms(c, backward, a, b, which, sid, s);
+  return backward ? layer_norm_backward(c, a, b, which, sid, s) : layer_norm(c, a, b, which, sid, s);
+}
+
+// Queries and keys of a packed [.][3 d] buffer turned in place.
+erase_status rope_qk(TfCtx* c, uint16_t* qkv, int backward, int b, int sid, hipStream_t s) {
+  const Layout& P = c->P;
+  const Dims& D = P.D;
+  if (!P.O.rope) return ERASE_OK;
+  RopeArgs a{};
+  for (int w = 0; w < 2; ++w) {
+    a.x[w] = a.y[w] = qkv + w * D.d;
+    a.xs[w][0] = a.ys[w][0] = int64_t(D.T) * P.ld3;
+    a.xs[w][1] = a.ys[w][1] = P.ld3;
+    a.xs[w][2] = a.ys[w][2] = 64;
+    a.heads[w] = D.H;
+  }
+  a.batch = D.B;
+  a.seq = D.T;
+  a.dim = 64;
+  a.rot = P.O.o.rope_spec.rot_dim;
+  a.start_t = 1;
+  a.table = P.rope;
+  a.interleaved = P.O.o.rope_layout == ERASE_ROPE_INTERLEAVED;
+  a.inverse = backward;
+  TFRUN(c, 18, b, backward, sid, 0.0, double(D.N) * 2 * D.H * a.rot * 4, 0, [&](const LaunchEv&) { return launch_rope(1, a, s); },
+        0, 0, 0, false, s);
+  return ERASE_OK;
+}
+
+// Dropout of a branch (0 attention, 1 MLP): forward y = res + drop(branch);
+// backward (res null) the gradient at the branch from that at y.
+erase_status drop(TfCtx* c, int branch, const uint16_t* x, const uint16_t* res, uint16_t* y, int b, int sid, hipStream_t s) {
+  const Layout& P = c->P;
+  if (!P.O.drop) return ERASE_OK;
+  DropArgs a{};
+  a.x = x;
+  a.res = res;
+  a.y = y;
+  a.ldx = a.ldres = a.ldy = P.ldd;
+  a.rows = P.D.N;
+  a.cols = P.D.d;
+  a.seed = P.O.o.seed;
+  a.offset = uint64_t(2 * b + branch) << 40;
+  a.step = reinterpret_cast<const uint64_t*>(P.t);
+  drop_rate(P.O.o.dropout, &a);
+  TFRUN(c, 19, b, branch + (res ? 0 : 2), sid, 0.0, double(P.D.N) * P.D.d * (res ? 6 : 4), 0,
+        [&](const LaunchEv&) { return launch_dropout(1, a, s); }, 0, 0, 0, false, s);
+  return ERASE_OK;
+}
+
 TfAttnArgs attn_args(const Layout& P, const Block& B) {
   TfAttnArgs a{};
   a.qkv = B.qkv;
@@ -598,15 +780,18 @@ erase_status enqueue_body(TfCtx* c, int b, const int32_t* tokens, hipStream_t s,
     TFRUN(c, 11, b, -1, sid, 0.0, double(D.N) * (4.0 * D.d + 8.0), (int)cdv(D.N, 4),
           [&](const LaunchEv& ev) { return launch_tf_embed(e, s, ev); });
   }
-  if (auto st = rms(c, 0, rms_args(P, B.a0, B.r1, B.n1), b, 0, sid, s); st != ERASE_OK) return st;
+  if (auto st = norm(c, 0, rms_args(P, B.a0, B.r1, B.n1), b, 0, sid, s); st != ERASE_OK) return st;
   if (auto st = gemm(c, B.fwd[WQKV], 1, b, WQKV, sid, s); st != ERASE_OK) return st;
+  if (auto st = rope_qk(c, B.qkv, 0, b, sid, s); st != ERASE_OK) return st;
   const TfAttnArgs at = attn_args(P, B);
   TFRUN(c, 14, b, 0, sid, 2.0 * attn_flops(D), 0.0, (int)(cdv(D.T, 64) * D.H * D.B),
         [&](const LaunchEv& ev) { return launch_tf_attn(0, at, s, ev); });
   if (auto st = gemm(c, B.fwd[WO], 1, b, WO, sid, s); st != ERASE_OK) return st;
-  if (auto st = rms(c, 0, rms_args(P, B.a1, B.r2, B.n2), b, 1, sid, s); st != ERASE_OK) return st;
+  if (auto st = drop(c, 0, P.branch, B.a0, B.a1, b, sid, s); st != ERASE_OK) return st;
+  if (auto st = norm(c, 0, rms_args(P, B.a1, B.r2, B.n2), b, 1, sid, s); st != ERASE_OK) return st;
   if (auto st = gemm(c, B.fwd[W1], 1, b, W1, sid, s); st != ERASE_OK) return st;
   if (auto st = gemm(c, B.fwd[W2], 1, b, W2, sid, s); st != ERASE_OK) return st;
+  if (auto st = drop(c, 1, P.branch, B.a1, B.z, b, sid, s); st != ERASE_OK) return st;
   return ERASE_OK;
 }
 
@@ -623,7 +808,7 @@ erase_status enqueue_head(TfCtx* c, int b, hipStream_t s, int sid) {
   ra.ldhw = D.cols[WH];
   ra.target = P.target;
   ra.xref = B.xref;
-  if (auto st = rms(c, 0, ra, b, 2, sid, s); st != ERASE_OK) return st;
+  if (auto st = norm(c, 0, ra, b, 2, sid, s); st != ERASE_OK) return st;
   if (auto st = gemm(c, B.fwd[WH], 1, b, WH, sid, s); st != ERASE_OK) return st;
   TfHeadArgs x{};
   x.e = B.logits;
@@ -686,8 +871,9 @@ erase_status enqueue_backward(TfCtx* c, int b, hipStream_t s, int sid) {
       a.ppstride = D.N * int64_t(D.d);
       a.npart = B.hsplit;
     }
-    if ((st = rms(c, 1, a, b, 2, sid, s)) != ERASE_OK) return st;
+    if ((st = norm(c, 1, a, b, 2, sid, s)) != ERASE_OK) return st;
   }
+  if ((st = drop(c, 1, B.dz, nullptr, P.dbranch, b, sid, s)) != ERASE_OK) return st;
   if ((st = G(B.dgr[W2], 4, W2)) != ERASE_OK) return st;
   if ((st = G(B.wgr[W2], 3, W2)) != ERASE_OK) return st;
   if ((st = G2(W1)) != ERASE_OK) return st;
@@ -697,12 +883,14 @@ erase_status enqueue_backward(TfCtx* c, int b, hipStream_t s, int sid) {
     a.lddy = P.ldd;
     a.res = B.dz;
     a.ldres = P.ldd;
-    if ((st = rms(c, 1, a, b, 1, sid, s)) != ERASE_OK) return st;
+    if ((st = norm(c, 1, a, b, 1, sid, s)) != ERASE_OK) return st;
   }
+  if ((st = drop(c, 0, B.da1, nullptr, P.dbranch, b, sid, s)) != ERASE_OK) return st;
   if ((st = G2(WO)) != ERASE_OK) return st;
   const TfAttnArgs at = attn_args(P, B);
   TFRUN(c, 15, b, 0, sid, 7.0 * attn_flops(D), 0.0, (int)(2 * cdv(D.T, 64) * D.H * D.B),
         [&](const LaunchEv& ev) { return launch_tf_attn(1, at, s, ev); });
+  if ((st = rope_qk(c, B.dqkv, 1, b, sid, s)) != ERASE_OK) return st;
   if (b == 0) {
     if ((st = G2(WQKV)) != ERASE_OK) return st;
     TfRmsArgs a = rms_args(P, B.a0, B.r1, nullptr);
@@ -712,7 +900,7 @@ erase_status enqueue_backward(TfCtx* c, int b, hipStream_t s, int sid) {
     a.ldres = P.ldd;
     a.out_f32 = B.da0;
     a.ldout = P.ldd;
-    if ((st = rms(c, 1, a, b, 0, sid, s)) != ERASE_OK) return st;
+    if ((st = norm(c, 1, a, b, 0, sid, s)) != ERASE_OK) return st;
     TfEmbGradArgs e{};
     e.input = P.input;
     e.N = D.N;
@@ -729,6 +917,12 @@ erase_status enqueue_backward(TfCtx* c, int b, hipStream_t s, int sid) {
     e.ldgrad = D.d;
     TFRUN(c, 17, b, -1, sid, 0.0, double(D.N) * D.d * 4.0 + double(D.V) * D.d * 4.0, (int)cdv(D.V, 4),
           [&](const LaunchEv&) { return launch_tf_emb_grad(e, s); }, 0, 0, 0, false, s);
+  } else if (P.O.layer) {  // g1 and b1 alone: nothing goes into the block's input
+    if ((st = G2(WQKV)) != ERASE_OK) return st;
+    TfRmsArgs a = rms_args(P, B.a0, B.r1, nullptr);
+    a.dy = P.dn1;
+    a.lddy = P.ldd;
+    if ((st = norm(c, 1, a, b, 0, sid, s)) != ERASE_OK) return st;
   } else if ((st = G(B.wgr[WQKV], 3, WQKV)) != ERASE_OK) {
     return st;
   }
@@ -820,27 +1014,48 @@ TfCtx* as_ctx(erase_tf_ctx* p) { return p ? &p->impl : nullptr; }
 
 extern "C" {
 
-erase_status erase_tf_param_count(const erase_tf_config* cfg, int32_t block, int64_t* count) {
+erase_status erase_tf_param_count_options(const erase_tf_config* cfg, const erase_tf_options* opt, int32_t block,
+                                          int64_t* count) {
   if (!count) return ERASE_ERR_INVALID_ARG;
   if (erase_status st = validate(cfg, nullptr); st != ERASE_OK) return st;
+  Opts O;
+  if (erase_status st = validate_options(opt, &O); st != ERASE_OK) return st;
   if (block < 0 || block >= cfg->n_layers) return ERASE_ERR_INVALID_ARG;
-  *count = param_count(dims_of(*cfg), block);
+  *count = param_count(dims_of(*cfg), O, block);
+  return ERASE_OK;
+}
+
+erase_status erase_tf_param_count(const erase_tf_config* cfg, int32_t block, int64_t* count) {
+  return erase_tf_param_count_options(cfg, nullptr, block, count);
+}
+
+erase_status erase_tf_workspace_bytes_options(const erase_tf_config* cfg, const erase_tf_options* opt, size_t* bytes) {
+  if (!bytes) return ERASE_ERR_INVALID_ARG;
+  if (erase_status st = validate(cfg, nullptr); st != ERASE_OK) return st;
+  Opts O;
+  if (erase_status st = validate_options(opt, &O); st != ERASE_OK) return st;
+  Layout P;
+  *bytes = build_layout(*cfg, O, 0, &P);
   return ERASE_OK;
 }
 
 erase_status erase_tf_workspace_bytes(const erase_tf_config* cfg, size_t* bytes) {
-  if (!bytes) return ERASE_ERR_INVALID_ARG;
-  if (erase_status st = validate(cfg, nullptr); st != ERASE_OK) return st;
-  Layout P;
-  *bytes = build_layout(*cfg, 0, &P);
-  return ERASE_OK;
+  return erase_tf_workspace_bytes_options(cfg, nullptr, bytes);
 }
 
 erase_status erase_tf_init(const erase_tf_config* cfg, const erase_block_buffers* bufs, void* workspace,
                            size_t ws_bytes, void* s_fwd, void* s_bwd, erase_tf_ctx** ctx_out) {
+  return erase_tf_init_options(cfg, nullptr, bufs, workspace, ws_bytes, s_fwd, s_bwd, ctx_out);
+}
+
+erase_status erase_tf_init_options(const erase_tf_config* cfg, const erase_tf_options* opt,
+                                   const erase_block_buffers* bufs, void* workspace, size_t ws_bytes, void* s_fwd,
+                                   void* s_bwd, erase_tf_ctx** ctx_out) {
   if (!ctx_out) return ERASE_ERR_INVALID_ARG;
   *ctx_out = nullptr;
   if (erase_status st = validate(cfg, nullptr); st != ERASE_OK) return st;
+  Opts O;
+  if (erase_status st = validate_options(opt, &O); st != ERASE_OK) return st;
   if (!bufs) return ERASE_ERR_INVALID_ARG;
   for (int b = 0; b < cfg->n_layers; ++b) {
     if (!bufs[b].param || !bufs[b].m || !bufs[b].v) return ERASE_ERR_INVALID_ARG;
@@ -852,7 +1067,7 @@ erase_status erase_tf_init(const erase_tf_config* cfg, const erase_block_buffers
   if (!workspace || reinterpret_cast<uintptr_t>(workspace) % kAlign) return ERASE_ERR_WORKSPACE;
   {
     Layout probe;
-    if (ws_bytes < build_layout(*cfg, 0, &probe)) return ERASE_ERR_WORKSPACE;
+    if (ws_bytes < build_layout(*cfg, O, 0, &probe)) return ERASE_ERR_WORKSPACE;
   }
   erase_tf_ctx* h = new erase_tf_ctx();
   TfCtx* c = &h->impl;
@@ -860,7 +1075,7 @@ erase_status erase_tf_init(const erase_tf_config* cfg, const erase_block_buffers
   c->ws = static_cast<char*>(workspace);
   c->sf = static_cast<hipStream_t>(s_fwd);
   c->sb = static_cast<hipStream_t>(s_bwd);
-  build_layout(c->cfg, reinterpret_cast<uintptr_t>(workspace), &c->P);
+  build_layout(c->cfg, O, reinterpret_cast<uintptr_t>(workspace), &c->P);
   build_gemms(c->cfg, &c->P);
   build_segments(&c->P, bufs);
   auto bail = [&](erase_status s) {
@@ -886,6 +1101,7 @@ erase_status erase_tf_init(const erase_tf_config* cfg, const erase_block_buffers
     if (hipMemcpyAsync(B.segs_dev, B.segs.data(), sizeof(AdamSeg) * B.segs.size(), hipMemcpyHostToDevice, c->sf) !=
         hipSuccess)
       return bail(ERASE_ERR_HIP);
+  if (O.rope && erase_rope_table(&O.o.rope_spec, c->P.rope, s_fwd) != ERASE_OK) return bail(ERASE_ERR_HIP);
   if (refresh(c) != ERASE_OK) return bail(ERASE_ERR_HIP);
   *ctx_out = h;
   return ERASE_OK;

@@ -8,16 +8,16 @@ is no fallback: without the library or a GPU the constructor raises.
 from __future__ import annotations
 
 import ctypes
-from ctypes import POINTER, c_float, c_int32, c_int64, c_size_t, c_void_p
+from ctypes import POINTER, c_double, c_float, c_int32, c_int64, c_size_t, c_uint64, c_void_p
 
 import numpy as np
 
-from . import erase, synth_tf
+from . import erase, erase_ops, synth_tf
 from .erase import BlockBuffers, EraseError, KernelTime, OK
 
 TF_KERNEL_KINDS = {0: "prologue", 1: "fwd_gemm", 3: "wgrad_gemm", 4: "dgrad_gemm", 5: "adam", 6: "bwd_gemm", 7: "empty",
                    11: "embed", 12: "rms_fwd", 13: "rms_bwd", 14: "attn_fwd", 15: "attn_bwd", 16: "head_norm",
-                   17: "emb_grad"}
+                   17: "emb_grad", 18: "rope", 19: "dropout"}
 GEMM_NAMES = {0: "qkv", 1: "proj", 2: "mlp_up", 3: "mlp_down", 4: "vocab"}
 SCHEDULES = {"serial": erase.SERIAL, "overlap": erase.OVERLAP}
 TENSORS = {"a0": 0, "n1": 1, "qkv": 2, "o": 3, "a1": 4, "n2": 5, "u": 6, "g": 7, "z": 8, "hn": 9,
@@ -30,7 +30,17 @@ class TfConfig(ctypes.Structure):
                 ("beta2", c_float), ("eps", c_float), ("lam", c_float)]
 
 
+class TfOptions(ctypes.Structure):
+    """erase_tf_options: what the blocks have beside the plain step."""
+    _fields_ = [("rope", c_int32), ("rope_layout", c_int32), ("rope_spec", erase_ops.RopeSpec), ("norm", c_int32),
+                ("norm_eps", c_float), ("dropout", c_double), ("seed", c_uint64)]
+
+
 SIGNATURES = {
+    "erase_tf_param_count_options": (c_int32, [POINTER(TfConfig), POINTER(TfOptions), c_int32, POINTER(c_int64)]),
+    "erase_tf_workspace_bytes_options": (c_int32, [POINTER(TfConfig), POINTER(TfOptions), POINTER(c_size_t)]),
+    "erase_tf_init_options": (c_int32, [POINTER(TfConfig), POINTER(TfOptions), POINTER(BlockBuffers), c_void_p, c_size_t,
+                                        c_void_p, c_void_p, POINTER(c_void_p)]),
     "erase_tf_param_count": (c_int32, [POINTER(TfConfig), c_int32, POINTER(c_int64)]),
     "erase_tf_workspace_bytes": (c_int32, [POINTER(TfConfig), POINTER(c_size_t)]),
     "erase_tf_init": (c_int32, [POINTER(TfConfig), POINTER(BlockBuffers), c_void_p, c_size_t, c_void_p, c_void_p,
@@ -74,17 +84,42 @@ def native_config(cfg: dict) -> TfConfig:
                     ad["beta1"], ad["beta2"], ad["eps"], float(cfg.get("lam", 1.0)))
 
 
+NORMS = {"rms": 0, "layer": 1}
+
+
+def native_options(cfg: dict) -> TfOptions | None:
+    """The options of a description (synth_tf); None where it has none."""
+    r, norm, p = cfg.get("rope"), cfg.get("norm", "rms"), cfg.get("dropout", 0.0)
+    if r is None and norm == "rms" and p == 0.0:
+        return None
+    o = TfOptions(rope=0 if r is None else 1, norm=NORMS[norm], norm_eps=cfg.get("norm_eps", 1e-5), dropout=p,
+                  seed=cfg.get("dropout_seed", 0))
+    if r is not None:
+        o.rope_layout = erase_ops.LAYOUTS[r.get("layout", "half")]
+        o.rope_spec = erase_ops.RopeSpec(r["rot_dim"], erase_ops.SCALINGS[r.get("scaling", "none")], r.get("base", 10000.0),
+                                         r.get("factor", 1.0), r.get("original_length", 0.0), r.get("fast", 32.0),
+                                         r.get("slow", 1.0))
+    return o
+
+
+def _options_ptr(cfg: dict):
+    o = native_options(cfg)
+    return None if o is None else ctypes.byref(o)
+
+
 def param_count(cfg: dict, block: int) -> int:
     n = c_int64(0)
     nc = native_config(cfg)
-    _check(lib().erase_tf_param_count(ctypes.byref(nc), block, ctypes.byref(n)), "erase_tf_param_count")
+    _check(lib().erase_tf_param_count_options(ctypes.byref(nc), _options_ptr(cfg), block, ctypes.byref(n)),
+           "erase_tf_param_count_options")
     return n.value
 
 
 def workspace_bytes(cfg: dict) -> int:
     n = c_size_t(0)
     nc = native_config(cfg)
-    _check(lib().erase_tf_workspace_bytes(ctypes.byref(nc), ctypes.byref(n)), "erase_tf_workspace_bytes")
+    _check(lib().erase_tf_workspace_bytes_options(ctypes.byref(nc), _options_ptr(cfg), ctypes.byref(n)),
+           "erase_tf_workspace_bytes_options")
     return n.value
 
 
@@ -124,9 +159,9 @@ class TfTrainer:
         self.sb = torch.cuda.Stream(device=self.dev)
         torch.cuda.synchronize(self.dev)
         ctx = c_void_p()
-        _check(lib().erase_tf_init(ctypes.byref(self.nc), bufs, c_void_p(self.ws_ptr), self.ws_bytes,
-                                   c_void_p(self.sf.cuda_stream), c_void_p(self.sb.cuda_stream), ctypes.byref(ctx)),
-               "erase_tf_init")
+        _check(lib().erase_tf_init_options(ctypes.byref(self.nc), _options_ptr(cfg), bufs, c_void_p(self.ws_ptr),
+                                           self.ws_bytes, c_void_p(self.sf.cuda_stream), c_void_p(self.sb.cuda_stream),
+                                           ctypes.byref(ctx)), "erase_tf_init_options")
         self.ctx = ctx
         if step:
             self.set_step(step)

@@ -18,8 +18,16 @@ Description (plain dict):
     {"name", "vocab", "d", "heads", "layers", "seq", "batch", "lam",
      "adam": {"lr", "beta1", "beta2", "eps"}}
 
+and, each optional (what the blocks have beside the plain step):
+
+    "rope":    {"rot_dim", "layout": "half" | "interleaved", "base", "scaling",
+                "factor", "original_length", "fast", "slow"} (rot_dim required)
+    "norm":    "rms" (default) | "layer", with "norm_eps" (default 1e-5)
+    "dropout": p of both branches, with "dropout_seed" (default 0)
+
 Parameters: one dict per block with ``wqkv`` [3d, d], ``wo`` [d, d],
-``w1`` [4d, d], ``w2`` [d, 4d], ``wh`` [V, d], and ``emb`` [V, d] in block 1.
+``w1`` [4d, d], ``w2`` [d, 4d], ``wh`` [V, d], and ``emb`` [V, d] in block 1; with
+layer norms also ``g1``, ``b1``, ``g2``, ``b2``, ``g3``, ``b3`` [d], drawn after the others.
 Random draw order for one seed: block 1's embedding, then per block wqkv,
 wo, w1, w2, wh, then the token batches.  Every parameter is drawn in
 float64 and rounded once to bf16 values (the workload is bf16), and the same
@@ -32,6 +40,7 @@ import numpy as np
 from .synth import ADAM_DEFAULT, round_to_bf16_values
 
 PARAM_ORDER = ("emb", "wqkv", "wo", "w1", "w2", "wh")
+NORM_ORDER = ("g1", "b1", "g2", "b2", "g3", "b3")
 
 
 def tf_config(name: str, **over) -> dict:
@@ -51,7 +60,8 @@ def param_shapes(cfg: dict, block: int) -> list:
     """[(name, shape)] of one block in flat order."""
     V, d = cfg["vocab"], cfg["d"]
     out = [("emb", (V, d))] if block == 0 else []
-    return out + [("wqkv", (3 * d, d)), ("wo", (d, d)), ("w1", (4 * d, d)), ("w2", (d, 4 * d)), ("wh", (V, d))]
+    out += [("wqkv", (3 * d, d)), ("wo", (d, d)), ("w1", (4 * d, d)), ("w2", (d, 4 * d)), ("wh", (V, d))]
+    return out + [(n, (d,)) for n in NORM_ORDER] if cfg.get("norm", "rms") == "layer" else out
 
 
 def param_count(cfg: dict, block: int) -> int:
@@ -60,7 +70,8 @@ def param_count(cfg: dict, block: int) -> int:
 
 def make_params(cfg: dict, rng: np.random.Generator, round_bf16: bool = True) -> list:
     """Embedding ~ N(0, 1) (``nn.Embedding``'s default), linear weights
-    ~ U(+-1/sqrt(fan_in)) (``nn.Linear``'s default), no biases."""
+    ~ U(+-1/sqrt(fan_in)) (``nn.Linear``'s default), no biases; a layer norm's
+    weight ~ N(1, 0.2^2) and bias ~ N(0, 0.2^2), as in a network under training."""
     rnd = round_to_bf16_values if round_bf16 else (lambda a: np.asarray(a, dtype=np.float32))
     out = []
     for b in range(cfg["layers"]):
@@ -68,6 +79,8 @@ def make_params(cfg: dict, rng: np.random.Generator, round_bf16: bool = True) ->
         for name, shape in param_shapes(cfg, b):
             if name == "emb":
                 a = rng.normal(0.0, 1.0, size=shape)
+            elif name in NORM_ORDER:
+                a = rng.normal(1.0 if name[0] == "g" else 0.0, 0.2, size=shape)
             else:
                 bound = 1.0 / np.sqrt(shape[1])
                 a = rng.uniform(-bound, bound, size=shape)
