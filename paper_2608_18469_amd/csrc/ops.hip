@@ -289,8 +289,9 @@ hipError_t launch_rope(int bf16, const RopeArgs& args, hipStream_t s) {
   // in bf16: 17.2 us; with two or four units a thread 18.7), fewer where that
   // leaves less than two workgroups a compute unit
   p.tokens = std::max(1, std::min({256 / per_token, kRopePairs / half, a.seq}));
-  while (p.tokens > 1 && (int64_t)a.batch * ((a.seq + p.tokens - 1) / p.tokens) < 512) p.tokens = (p.tokens + 1) / 2;
-  p.row_groups = (uint32_t)((a.seq + p.tokens - 1) / p.tokens);
+  auto row_groups = [&] { return ((int64_t)a.seq + p.tokens - 1) / p.tokens; };
+  while (p.tokens > 1 && a.batch * row_groups() < 512) p.tokens = (p.tokens + 1) / 2;
+  p.row_groups = (uint32_t)row_groups();
   p.groups = (uint32_t)a.batch * p.row_groups;
   const uint32_t grid = std::min<uint32_t>(p.groups, 1 << 20);
   const uint32_t splits = (uint32_t)((per_token + 1023) / 1024);  // of one token's heads, beyond four units a thread
@@ -957,7 +958,7 @@ __global__ __launch_bounds__(256) void ops_dropout(DropPlan p) {
 hipError_t launch_dropout(int bf16, const DropArgs& args, hipStream_t s) {
   DropPlan p{};
   p.a = args;
-  p.groups = fast_div((uint32_t)((args.cols + 7) / 8));
+  p.groups = fast_div((uint32_t)(((int64_t)args.cols + 7) / 8));
   // threads are numbered in 32 bits: that many rows a launch
   const int64_t slab = std::max<int64_t>(1, (int64_t(1) << 31) / p.groups.d);
   for (int64_t r = 0; r < args.rows; r += slab) {

@@ -512,6 +512,26 @@ def test_dropout_of_more_than_2_to_the_32_elements():
         assert np.array_equal(x[r].float().cpu().numpy() > 0, words[0]), r
 
 
+def test_the_longest_sequence_and_row():
+    """2^31 - 1 positions in one sequence, 2^31 - 1 columns in one row."""
+    import torch
+    n = (1 << 31) - 1
+    print("[longest] rope", flush=True)
+    x = torch.ones((1, n, 1, 2), dtype=torch.bfloat16, device="cuda")
+    at = [0, 1, 12345, 1 << 30, n - 2, n - 1]
+    ops.rope(x, None, ops.rope_table(2), out=(x, None))
+    got = _np(x[:, at])
+    _check_rope(got, np.ones_like(got), np.array([at]), dict(rot_dim=2), "half", 1.0, "bf16", "longest")
+    del x
+    print("[longest] dropout", flush=True)
+    x = torch.ones((1, n), dtype=torch.bfloat16, device="cuda")
+    ops.dropout(x, 0.5, 3, out=x)
+    group = n // 8  # of the last columns
+    words = oo.philox(np.array([[group, 0, 0, 0]], np.uint64), (3, 0))[0]
+    halves = np.stack([words & 0xFFFF, words >> 16], -1).reshape(-1)
+    assert np.array_equal(_np(x[0, 8 * group:]) > 0, (halves >= 32768)[:n - 8 * group])
+
+
 def test_layer_norm_of_more_rows_than_one_grid_row_takes():
     """2^26 + 5 rows, a wave each: 2^32 threads and more."""
     import torch
