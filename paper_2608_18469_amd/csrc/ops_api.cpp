@@ -103,7 +103,8 @@ erase_status rope(const erase_rope_config* cfg, const void* q, const void* k, vo
   if (!known(c.dtype) || c.layout < ERASE_ROPE_HALF || c.layout > ERASE_ROPE_INTERLEAVED) return ERASE_ERR_INVALID_ARG;
   if (c.batch < 0 || c.seq < 0 || int64_t(c.batch) * c.seq >= kRows || c.q_heads < 1 || c.q_heads > 4096 ||
       c.k_heads < 0 || c.k_heads > 4096 || c.head_dim > 1024 || c.rot_dim < 2 || c.rot_dim % 2 ||
-      c.rot_dim > c.head_dim || c.pos_stride < 0 || c.pos_stride >= kSpan / kRows)
+      c.rot_dim > c.head_dim || c.pos_stride < 0 ||
+      (c.batch > 1 && static_cast<__int128>(c.batch) * c.pos_stride >= kSpan))
     return ERASE_ERR_SHAPE;
   if (c.start < -(int64_t(1) << 40) || c.start > (int64_t(1) << 40)) return ERASE_ERR_INVALID_ARG;
   const int64_t nq[3] = {c.batch, c.seq, c.q_heads}, nk[3] = {c.batch, c.seq, c.k_heads};

@@ -83,7 +83,8 @@ def _rope(fn="erase_rope", q=P, k=Q, qo=R, ko=S, pos=None, table=P, **kw):
     (dict(dtype=2), INVALID), (dict(dtype=-1), INVALID), (dict(layout=2), INVALID), (dict(layout=-1), INVALID),
     (dict(batch=-1), SHAPE), (dict(seq=-1), SHAPE), (dict(batch=1 << 16, seq=1 << 15), SHAPE), (dict(q_heads=0), SHAPE),
     (dict(q_heads=4097), SHAPE), (dict(k_heads=-1), SHAPE), (dict(head_dim=1026), SHAPE), (dict(rot_dim=0), SHAPE),
-    (dict(rot_dim=63), SHAPE), (dict(rot_dim=66), SHAPE), (dict(pos_stride=-1), SHAPE), (dict(start=1 << 41), INVALID),
+    (dict(rot_dim=63), SHAPE), (dict(rot_dim=66), SHAPE), (dict(pos_stride=-1), SHAPE), (dict(pos_stride=1 << 48), SHAPE),
+    (dict(start=1 << 41), INVALID),
     (dict(start=-(1 << 41)), INVALID), (dict(q_stride=(-768, 256, 64)), SHAPE), (dict(k_stride=(384, 128, -64)), SHAPE),
     (dict(q_stride=(1 << 62, 256, 64)), SHAPE),                  # beyond any memory
     (dict(qo_stride=(768, 256, 32)), SHAPE),                     # heads of the output overlap

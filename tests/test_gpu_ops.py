@@ -167,6 +167,21 @@ def test_rope_of_a_packed_projection_and_of_nothing():
         assert qo.shape == e.shape and ko.shape == e.shape
 
 
+def test_rope_positions_of_long_rows():
+    """Rows of positions 200000 apart, and a single row whose stride says nothing."""
+    import torch
+    T = 200000
+    table = ops.rope_table(2)
+    x = torch.ones((2, T, 1, 2), device="cuda")
+    pos = torch.arange(2 * T, dtype=torch.int32, device="cuda").view(2, T)
+    at = [0, 1, 131071, 131072, T - 1]
+    y, _ = ops.rope(x, None, table, positions=pos)
+    got = _np(y[:, at])
+    _check_rope(got, np.ones_like(got), _np(pos[:, at]), dict(rot_dim=2), "half", 1.0, "f32", "long rows")
+    y1, _ = ops.rope(x[:1], None, table, positions=pos.view(-1)[:T].as_strided((1, T), (1 << 40, 1)))
+    assert torch.equal(y1, y[:1])
+
+
 def test_rope_broadcast_input_and_infinities():
     import torch
     x, ref = _dev(np.random.Generator(np.random.PCG64(6)).normal(size=(1, 1, 1, 64)), "f32")
