@@ -53,6 +53,7 @@ class DropoutConfig(ctypes.Structure):
 # The same three as packed bytes, for the calls themselves: a Structure with its
 # arrays costs 2 us more than one pack, of 8 to 12 us for a whole call.
 _ROPE, _NORM, _DROPOUT = struct.Struct("8i14q"), struct.Struct("qiif5q"), struct.Struct("qqidQQ3q")
+_UNPACKABLE = (struct.error, OverflowError)  # a number that its field does not hold
 assert (_ROPE.size, _NORM.size, _DROPOUT.size) == tuple(map(ctypes.sizeof, (RopeConfig, NormConfig, DropoutConfig)))
 
 # every entry point of include/erase_ops.h with its ctypes signature
@@ -114,14 +115,14 @@ def _on(where: str, *tensors) -> int:
     return dev
 
 
-def _like(where: str, name: str, t, x):
-    if t.dtype != x.dtype or t.shape != x.shape:
-        raise EraseError(ERR_SHAPE if t.dtype == x.dtype else ERR_INVALID_ARG, where,
-                         f"{name} must have the type {x.dtype} and the shape {list(x.shape)}")
+def _like(where: str, name: str, t, dtype, shape):
+    if t.dtype != dtype or t.shape != shape:
+        raise EraseError(ERR_SHAPE if t.dtype == dtype else ERR_INVALID_ARG, where,
+                         f"{name} must have the type {dtype} and the shape {list(shape)}")
 
 
 def _vector(where: str, name: str, t, n: int):
-    if t is not None and (t.dtype != torch.float32 or t.shape != (n,) or not t.is_contiguous()):
+    if t is not None and (t.dtype != torch.float32 or t.dim() != 1 or t.numel() != n or not t.is_contiguous()):
         raise EraseError(ERR_INVALID_ARG, where, f"{name} must be a contiguous float32 tensor of {n}")
 
 
@@ -144,13 +145,6 @@ def _run(where: str, fn, dev: int, stream, *args):
 
 def _ptr(t):
     return None if t is None else t.data_ptr()
-
-
-def _pack(where: str, form: struct.Struct, *values) -> bytes:
-    try:
-        return form.pack(*values)
-    except (struct.error, OverflowError) as e:
-        raise EraseError(ERR_SHAPE, where, str(e)) from None
 
 
 def _empty(shape, dtype, device, stream):
@@ -219,7 +213,7 @@ def _rotate(where, fn, q, k, table, positions, start, layout, out, stream):
     Hk, ks = 0, (0, 0, 0, 0)
     if k is not None:
         ks = _heads(where, "k", k)
-        Bk, Tk, Hk, Dk = k.shape
+        Bk, Tk, Hk, Dk = kshape = k.shape
         if k.dtype != q.dtype or Bk != B or Tk != T or Dk != D:
             raise EraseError(ERR_SHAPE, where, "k must have q's type, batch, length and head size")
     pos_stride = 0
@@ -230,18 +224,21 @@ def _rotate(where, fn, q, k, table, positions, start, layout, out, stream):
         pos_stride = ps[0]
     if out is None:
         qo = _empty(shape, q.dtype, q.device, stream)
-        ko = None if k is None else _empty(k.shape, k.dtype, k.device, stream)
+        ko = None if k is None else _empty(kshape, k.dtype, k.device, stream)
     else:
         qo, ko = out
         if qo is None or (ko is None) != (k is None):
             raise EraseError(ERR_INVALID_ARG, where, "out must give a tensor exactly where there is an input")
-        _like(where, "out[0]", qo, q)
+        _like(where, "out[0]", qo, q.dtype, shape)
         if k is not None:
-            _like(where, "out[1]", ko, k)
+            _like(where, "out[1]", ko, q.dtype, kshape)
     dev = _on(where, q, k, table.data, positions, qo, ko)
     qos = _heads(where, "out[0]", qo)
     kos = ks if k is None else _heads(where, "out[1]", ko)
-    cfg = _pack(where, _ROPE, dt, lay, B, T, Hq, Hk, D, table.rot_dim, *qs[:3], *ks[:3], *qos[:3], *kos[:3], pos_stride, start)
+    try:
+        cfg = _ROPE.pack(dt, lay, B, T, Hq, Hk, D, table.rot_dim, *qs[:3], *ks[:3], *qos[:3], *kos[:3], pos_stride, start)
+    except _UNPACKABLE as e:
+        raise EraseError(ERR_SHAPE, where, str(e)) from None
     _run(where, fn, dev, stream, cfg, q.data_ptr(), _ptr(k), qo.data_ptr(), _ptr(ko), _ptr(positions), table.data.data_ptr())
     return qo, ko
 
@@ -281,7 +278,7 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, out=None, stream=None):
     where = "erase_layer_norm"
     ld = _matrix(where, "x", x)
     dt = _dtype(where, "x", x)
-    R, C = x.shape
+    R, C = shape = x.shape
     _vector(where, "weight", weight, C)
     _vector(where, "bias", bias, C)
     if out is None:
@@ -289,11 +286,14 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, out=None, stream=None):
         mean, rstd = _empty((2, R), torch.float32, x.device, stream)
     else:
         y, mean, rstd = out
-        _like(where, "out[0]", y, x)
+        _like(where, "out[0]", y, x.dtype, shape)
         _vector(where, "out[1]", mean, R)
         _vector(where, "out[2]", rstd, R)
     dev = _on(where, x, weight, bias, y, mean, rstd)
-    cfg = _pack(where, _NORM, R, C, dt, eps, ld, _matrix(where, "out[0]", y), 0, 0, 0)
+    try:
+        cfg = _NORM.pack(R, C, dt, eps, ld, _matrix(where, "out[0]", y), 0, 0, 0)
+    except _UNPACKABLE as e:
+        raise EraseError(ERR_SHAPE, where, str(e)) from None
     _run(where, lib().erase_layer_norm, dev, stream, cfg, x.data_ptr(), _ptr(weight), _ptr(bias), y.data_ptr(), _ptr(mean),
          _ptr(rstd))
     return y, mean, rstd
@@ -310,7 +310,10 @@ def layer_norm_backward_scratch(x):
     every call in flight."""
     where = "erase_layer_norm_backward"
     _matrix(where, "x", x)
-    cfg = _pack(where, _NORM, x.shape[0], x.shape[1], _dtype(where, "x", x), 0.0, 0, 0, 0, 0, 0)
+    try:
+        cfg = _NORM.pack(x.shape[0], x.shape[1], _dtype(where, "x", x), 0.0, 0, 0, 0, 0, 0)
+    except _UNPACKABLE as e:
+        raise EraseError(ERR_SHAPE, where, str(e)) from None
     return torch.empty(_norm_scratch_bytes(cfg), dtype=torch.uint8, device=x.device)
 
 
@@ -324,8 +327,8 @@ def layer_norm_backward(dy, x, weight, mean, rstd, residual=None, need_input=Tru
     where = "erase_layer_norm_backward"
     ld = _matrix(where, "x", x)
     dt = _dtype(where, "x", x)
-    R, C = x.shape
-    _like(where, "dy", dy, x)
+    R, C = shape = x.shape
+    _like(where, "dy", dy, x.dtype, shape)
     _vector(where, "weight", weight, C)
     _vector(where, "mean", mean, R)
     _vector(where, "rstd", rstd, R)
@@ -335,7 +338,7 @@ def layer_norm_backward(dy, x, weight, mean, rstd, residual=None, need_input=Tru
     elif dx is None:
         dx = _empty((R, C), x.dtype, x.device, stream)
     else:
-        _like(where, "out[0]", dx, x)
+        _like(where, "out[0]", dx, x.dtype, shape)
     if not need_weight:
         dw = None
     elif dw is None:
@@ -349,10 +352,13 @@ def layer_norm_backward(dy, x, weight, mean, rstd, residual=None, need_input=Tru
     else:
         _vector(where, "out[2]", db, C)
     if residual is not None:
-        _like(where, "residual", residual, x)
-    cfg = _pack(where, _NORM, R, C, dt, 0.0, ld, 0, _matrix(where, "dy", dy),
-                0 if dx is None else _matrix(where, "out[0]", dx),
-                0 if residual is None else _matrix(where, "residual", residual))
+        _like(where, "residual", residual, x.dtype, shape)
+    try:
+        cfg = _NORM.pack(R, C, dt, 0.0, ld, 0, _matrix(where, "dy", dy),
+                    0 if dx is None else _matrix(where, "out[0]", dx),
+                    0 if residual is None else _matrix(where, "residual", residual))
+    except _UNPACKABLE as e:
+        raise EraseError(ERR_SHAPE, where, str(e)) from None
     if scratch is None:
         if need_weight or need_bias:
             scratch = _empty(_norm_scratch_bytes(cfg), torch.uint8, x.device, stream)
@@ -371,21 +377,24 @@ def layer_norm_backward(dy, x, weight, mean, rstd, residual=None, need_input=Tru
 def _drop(where, fn, x, p, seed, offset, residual, step, out, stream):
     ld = _matrix(where, "x", x)
     dt = _dtype(where, "x", x)
+    R, C = shape = x.shape
     if not (0 <= seed < 1 << 64 and 0 <= offset < 1 << 64):
         raise EraseError(ERR_INVALID_ARG, where, "seed and offset must be 64-bit unsigned numbers")
     if step is not None and (step.dtype not in (torch.int64, torch.uint64) or step.numel() != 1):
         raise EraseError(ERR_INVALID_ARG, where, "step must be one int64 or uint64 on the device")
     if out is None:
-        out = _empty(x.shape, x.dtype, x.device, stream)
+        out = _empty(shape, x.dtype, x.device, stream)
     else:
-        _like(where, "out", out, x)
+        _like(where, "out", out, x.dtype, shape)
     lr = 0
     if residual is not None:
-        _like(where, "residual", residual, x)
+        _like(where, "residual", residual, x.dtype, shape)
         lr = _matrix(where, "residual", residual)
     dev = _on(where, x, residual, step, out)
-    R, C = x.shape
-    cfg = _pack(where, _DROPOUT, R, C, dt, p, seed, offset, ld, lr, _matrix(where, "out", out))
+    try:
+        cfg = _DROPOUT.pack(R, C, dt, p, seed, offset, ld, lr, _matrix(where, "out", out))
+    except _UNPACKABLE as e:
+        raise EraseError(ERR_SHAPE, where, str(e)) from None
     if fn == "erase_dropout":
         _run(where, lib().erase_dropout, dev, stream, cfg, x.data_ptr(), _ptr(residual), out.data_ptr(), _ptr(step))
     else:
