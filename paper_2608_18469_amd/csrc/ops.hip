@@ -171,7 +171,8 @@ hipError_t launch_rope_fill(const RopeFillArgs& a, hipStream_t s) { return launc
 // their sines and cosines once into LDS, then its threads take units of those
 // tokens' heads, 32 bytes each: V pairs (two 16-byte chunks) or 2 V columns that
 // pass.  HBM bounds it: 671 MB read and written (32768 tokens of 40 heads of 128,
-// half of each turned) take 131 us, 5.1 TB/s.  Columns that pass in units of one
+// half of each turned) take 124 us, 5.4 TB/s (the rest of a copy's rate comes from
+// the cache).  Columns that pass in units of one
 // chunk, on a path of their own, took 163 us; several units' loads issued before
 // the sines 162 to 224 (the registers cost more waves than the loads hide).
 constexpr int kRopePairs = 2048;  // pairs of a workgroup's tokens (16 KB of LDS)
@@ -483,9 +484,7 @@ __global__ __launch_bounds__(S::threads) void ops_norm(NormArgs a) {
     const int64_t n = row ? n0 + grp : n0;  // (behind the last row: an existing one, not stored)
     Chunk<T> x[K];
 #pragma unroll
-    for (int i = 0; i < K; ++i) {
-      x[i] = ld_window<S>(static_cast<const T*>(a.x) + n * a.ldx, at[i]);
-    }
+    for (int i = 0; i < K; ++i) x[i] = ld_window<S>(static_cast<const T*>(a.x) + n * a.ldx, at[i]);
     float s = 0.f;
 #pragma unroll
     for (int i = 0; i < K; ++i) {
@@ -642,9 +641,9 @@ __device__ __forceinline__ NormRow<S, M> ld_norm_row(const NormBwdArgs& a, const
   return v;
 }
 
-// dw and db of 16 chunks of columns over all rows, 64 rows at a time: with few
-// rows these workgroups run beside those of dx (which has its row sums from the
-// forward's statistics either way), and no launch adds partial rows up.
+// dw and db of 16 chunks of columns over all rows, 64 rows at a time: they need
+// the forward's statistics but none of dx's sums, so with few rows these
+// workgroups run beside those of dx and no launch adds partial rows up.
 template <typename S>
 __device__ __forceinline__ void norm_strip(const NormBwdArgs& a, int strip, float* comb) {
   typedef typename S::T T;
@@ -688,10 +687,10 @@ __device__ __forceinline__ void norm_strip(const NormBwdArgs& a, int strip, floa
 // db in registers over all its rows.  At the end the workgroup's row groups are
 // added in order through LDS and one partial row per workgroup is stored (a
 // single workgroup stores dw and db themselves).  Workgroups of 1024 threads, one
-// a compute unit, keep the partial rows few: 16384 x 512 bf16 with res takes 19.7
-// us with 256 of them (4 of it the launch that adds them up), 23 with 512 of 256
-// threads, 31 with 256 of 256 (too few rows in flight).  16384 x 4096 takes 86.7
-// us, 4.6 TB/s.  The next row's loads are issued ahead where a row's
+// a compute unit, keep the partial rows few: 16384 x 512 bf16 with res takes 16.1
+// us and the launch that adds them up 3.9 (in all 23 with 512 of 256 threads, 31
+// with 256 of 256: too few rows in flight).  16384 x 4096 takes 79.6 and 4.9 us,
+// 5.1 TB/s.  The next row's loads are issued ahead where a row's
 // waves meet at a barrier (17495 x 1083: 42.9 us, 47.0 without; rows of one wave
 // lose up to a tenth by it).
 template <typename S, NormMode M>
@@ -798,7 +797,7 @@ __global__ __launch_bounds__(1024) void ops_norm_bwd(NormBwdArgs a) {
     }
   }
   if (!a.part) return;
-  const bool alone = a.nparts == 1;  // (the whole of dw and db)
+  const bool alone = a.nparts == 1;
   float* part = a.part + (int64_t)blockIdx.x * 2 * a.ldpart;
   st_norm_part<S>(aw, at, comb, grp, a.cols, alone ? a.dw : part);
   if constexpr (G > 1) __syncthreads();
@@ -914,7 +913,7 @@ __device__ __forceinline__ void philox(uint32_t x[4], uint32_t k0, uint32_t k1) 
 // A thread takes eight columns of a row: one counter, one or two chunks.  The
 // ten rounds are 20 products of 32 x 32 bits, which issue at a quarter of the
 // rate of an addition: 16 bits an element (rather than 32) keep them below the
-// time HBM needs.
+// time HBM needs.  16384 x 4096 bf16 takes 45.5 us for 268 MB read and written.
 struct DropPlan {
   DropArgs a;
   FastDiv groups;  // eights of a row

@@ -594,6 +594,62 @@ def test_two_streams_at_once():
             assert torch.equal(a, b)
 
 
+def test_two_host_threads_at_once():
+    """Calls of two threads, each on a stream of its own, share nothing."""
+    import threading
+
+    import torch
+    x = [torch.randn((700, 1000), device="cuda").bfloat16() for _ in range(2)]
+    q = torch.randn((4, 100, 4, 64), device="cuda")
+    table = ops.rope_table(64)
+    torch.cuda.synchronize()
+
+    def work(i, n):
+        out = []
+        for j in range(n):
+            y, m, r = ops.layer_norm(x[i])
+            out = [y, *ops.layer_norm_backward(x[1 - i], x[i], None, m, r), ops.rope(q, None, table, start=i)[0],
+                   ops.dropout(x[i], 0.3, i)]
+        return out
+
+    want = [work(i, 1) for i in range(2)]
+    torch.cuda.synchronize()
+    got = [None, None]
+
+    def run(i):
+        s = torch.cuda.Stream()
+        with torch.cuda.stream(s):
+            got[i] = work(i, 50)
+        s.synchronize()
+
+    ts = [threading.Thread(target=run, args=(i,)) for i in range(2)]
+    for t in ts:
+        t.start()
+    for t in ts:
+        t.join()
+    for a, b in zip(want, got):
+        assert b is not None and all(torch.equal(u, v) for u, v in zip(a, b))
+
+
+def test_named_stream_owns_what_is_allocated_for_it():
+    """With a stream given by name the outputs and the scratch come from that
+    stream's memory: the current stream's next allocations do not touch them."""
+    import torch
+    x, dy = torch.randn((3000, 512), device="cuda"), torch.randn((3000, 512), device="cuda")
+    w = torch.ones(512, device="cuda")
+    y0, m, r = ops.layer_norm(x, w)
+    want = ops.layer_norm_backward(dy, x, w, m, r)
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(20):
+        got = ops.layer_norm_backward(dy, x, w, m, r, stream=s)
+        junk = [torch.full((1 << 20,), float("nan"), device="cuda") for _ in range(4)]  # would reuse freed scratch
+        del junk
+    s.synchronize()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+
+
 def test_captured_and_replayed():
     """Forward and backward of the three in one graph: every replay equals the
     eager calls, with a new dropout mask whenever the counter moved."""
