@@ -286,10 +286,21 @@ hipError_t launch_rope(int bf16, const RopeArgs& args, hipStream_t s) {
   p.per_head = fast_div((uint32_t)per_head);
   p.per_token = fast_div((uint32_t)per_token);
   p.pairs = fast_div((uint32_t)half);
-  // as many tokens as give every thread one unit (16384 tokens of 16 heads of 64
-  // in bf16: 17.2 us; with two or four units a thread 18.7), fewer where that
-  // leaves less than two workgroups a compute unit
-  p.tokens = std::max(1, std::min({256 / per_token, kRopePairs / half, a.seq}));
+  // as many tokens as give every thread one unit, or two where that leaves fewer
+  // threads without any (57274 tokens of 144 units: 107 us with three tokens in
+  // two rounds, 129 to 137 with one token on 144 of 256 threads; more rounds hide
+  // less latency: tokens of 320 units 82 us in two rounds of one, 92 in five of four);
+  // fewer where that leaves less than two workgroups a compute unit
+  int best = 1;
+  double used = 0.0;  // share of the threads' rounds
+  for (int n = 1; n <= 2; ++n) {
+    const int t = 256 * n / per_token;
+    if (t >= 1 && double(t) * per_token / (256 * n) > used + 0.05) {
+      best = t;
+      used = double(t) * per_token / (256 * n);
+    }
+  }
+  p.tokens = std::max(1, std::min({best, kRopePairs / half, a.seq}));
   auto row_groups = [&] { return ((int64_t)a.seq + p.tokens - 1) / p.tokens; };
   while (p.tokens > 1 && a.batch * row_groups() < 512) p.tokens = (p.tokens + 1) / 2;
   p.row_groups = (uint32_t)row_groups();
