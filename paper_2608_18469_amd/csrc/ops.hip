@@ -113,7 +113,7 @@ __device__ __forceinline__ void st_chunk(T* p, int n, const float v[Chunk<T>::V]
   st_raw(p, n, pack_chunk<T>(v));
 }
 
-// Sum over groups of L = 16 or 64 lanes, the same bits in every lane: within 16
+// Sum over groups of L = 4, 16 or 64 lanes, the same bits in every lane: within 16
 // lanes by lane permutations in the add itself (xor 1, xor 2, mirrored halves,
 // mirrored rows), beyond by exchanging rows and halves.
 template <int CTRL>
@@ -124,8 +124,10 @@ template <int L>
 __device__ __forceinline__ float lane_sum(float v) {
   v += dpp<0xb1>(v);
   v += dpp<0x4e>(v);
-  v += dpp<0x141>(v);
-  v += dpp<0x140>(v);
+  if constexpr (L >= 16) {
+    v += dpp<0x141>(v);
+    v += dpp<0x140>(v);
+  }
   if constexpr (L == 64) {
     auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
@@ -314,8 +316,8 @@ hipError_t launch_rope(int bf16, const RopeArgs& args, hipStream_t s) {
 // ---------------------------------------------------------------------------
 // layer norm
 // ---------------------------------------------------------------------------
-// Layouts of the row kernels: a row is held by `lanes` threads (16 of a wave, a
-// wave, or W waves), K chunks of 16 bytes each; a workgroup of the forward takes
+// Layouts of the row kernels: a row is held by `lanes` threads (4 or 16 of a wave,
+// a wave, or W waves), K chunks of 16 bytes each; a workgroup of the forward takes
 // `groups` rows, one of the backward as many as 1024 threads hold.
 template <typename E, int Lanes, int Waves, int Chunks, bool Narrow = false>
 struct RowShape {
@@ -330,16 +332,18 @@ struct RowShape {
 namespace {
 
 // Calls f with the shape that holds a row of `cols` elements in the forward, and
-// in the backward (whose workgroups have 1024 threads).  The forward takes the
+// in the backward (whose workgroups have 1024 threads).  Narrow rows share a wave
+// (1196284 x 26 bf16: 32 us with 4 lanes a row, 89 with 16).  The forward takes the
 // fewest waves that hold the row with weight and bias: rows of a wave need no
-// barrier (16000 x 1500 bf16: 21.5 us with 3 chunks a lane, 25.6 with 4 waves), and
+// barrier (16000 x 1500: 21.5 us with 3 chunks a lane, 25.6 with 4 waves), and
 // several rows of a compute unit are in flight (3605 x 4160: 17.3 us with 4 waves
 // of 3 chunks, 25.5 with 16 of 1).  The backward holds three times as much a
 // column and takes one chunk a lane while it can.
 template <typename T, typename F>
 auto with_norm_shape(int cols, F&& f) {
   constexpr int V = Chunk<T>::V;
-  if (cols < V) return f(RowShape<T, 16, 1, 1, true>());
+  if (cols < V) return f(RowShape<T, 4, 1, 1, true>());
+  if (cols <= 4 * V) return f(RowShape<T, 4, 1, 1>());
   if (cols <= 16 * V) return f(RowShape<T, 16, 1, 1>());
   if (cols <= 64 * V) return f(RowShape<T, 64, 1, 1>());
   if (cols <= 128 * V) return f(RowShape<T, 64, 1, 2>());
@@ -355,7 +359,8 @@ auto with_norm_shape(int cols, F&& f) {
 template <typename T, typename F>
 auto with_norm_bwd_shape(int cols, F&& f) {
   constexpr int V = Chunk<T>::V;
-  if (cols < V) return f(RowShape<T, 16, 1, 1, true>());
+  if (cols < V) return f(RowShape<T, 4, 1, 1, true>());
+  if (cols <= 4 * V) return f(RowShape<T, 4, 1, 1>());
   if (cols <= 16 * V) return f(RowShape<T, 16, 1, 1>());
   if (cols <= 64 * V) return f(RowShape<T, 64, 1, 1>());
   if (cols <= 128 * V) return f(RowShape<T, 64, 2, 1>());
@@ -570,7 +575,8 @@ hipError_t launch_norm(int bf16, const NormArgs& a, hipStream_t s) {
 namespace {
 
 // A workgroup's sums of its rows' columns into `part` (NULL: not wanted), its
-// row groups added in order in LDS.
+// row groups added in order in LDS, in two stages where few threads have a column
+// (425494 x 32 bf16: 22.9 us, 32.1 in one).
 template <typename S, typename A>
 __device__ __forceinline__ void st_norm_part(const A& acc, const Window* at, float* comb, int grp, int cols, float* part) {
   constexpr int V = Chunk<typename S::T>::V;
@@ -580,12 +586,29 @@ __device__ __forceinline__ void st_norm_part(const A& acc, const Window* at, flo
 #pragma unroll
     for (int k = 0; k < V; ++k)
       if (k >= at[i].skip) (S::bwd_groups > 1 ? comb + grp * S::cols : part)[at[i].at + k] = acc[i][k];
-  if constexpr (S::bwd_groups > 1) {
+  if constexpr (S::bwd_groups > 1 && S::cols > 256) {
     __syncthreads();
     for (int c = threadIdx.x; c < cols; c += 1024) {
       float v = comb[c];
 #pragma unroll 4
       for (int g = 1; g < S::bwd_groups; ++g) v += comb[g * S::cols + c];
+      part[c] = v;
+    }
+  } else if constexpr (S::bwd_groups > 1) {  // many groups of few columns: slices of them, then the slices
+    constexpr int slices = 1024 / S::cols, per = S::bwd_groups / slices;
+    const int c = threadIdx.x % S::cols, slice = threadIdx.x / S::cols;
+    __syncthreads();
+    float v = 0.f;
+    if (c < cols)
+#pragma unroll
+      for (int g = 0; g < per; ++g) v += comb[(slice * per + g) * S::cols + c];
+    __syncthreads();
+    comb[threadIdx.x] = v;
+    __syncthreads();
+    if (slice == 0 && c < cols) {
+      v = 0.f;
+#pragma unroll 8
+      for (int g = 0; g < slices; ++g) v += comb[g * S::cols + c];
       part[c] = v;
     }
   }

@@ -242,7 +242,7 @@ def _norm_case(dtype, R, C, weight=True, bias=True, lead=0, gap=0, inplace=False
         assert _rest_untouched(yb, lead, R, C, ld), what
 
 
-COLS = [1, 2, 7, 8, 9, 63, 64, 65, 127, 128, 129, 255, 256, 257, 401, 511, 512, 513, 1000, 1023, 1024, 1025, 1677, 2047, 2048, 2049,
+COLS = [1, 2, 3, 4, 5, 7, 8, 9, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 255, 256, 257, 401, 511, 512, 513, 1000, 1023, 1024, 1025, 1677, 2047, 2048, 2049,
         4096, 4097, 8191, 8192, 8193, 12345, 16383, 16384]
 
 
@@ -364,7 +364,7 @@ def test_layer_norm_backward_widths(dtype, C):
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("R,C", [(0, 64), (1, 1), (2, 512), (3, 100), (63, 64), (257, 512), (1000, 130), (4099, 40), (2051, 520),
-                                 (1500, 1100), (700, 4096), (5000, 16)])
+                                 (1500, 1100), (700, 4096), (5000, 16), (70001, 26), (9000, 6), (33000, 31)])
 def test_layer_norm_backward_rows(dtype, R, C):
     _norm_bwd_case(dtype, R, C, weight=R % 2 == 0, res=R % 3 == 0)
 
