@@ -113,9 +113,9 @@ __device__ __forceinline__ void st_chunk(T* p, int n, const float v[Chunk<T>::V]
   st_raw(p, n, pack_chunk<T>(v));
 }
 
-// Sum over groups of L = 4, 16 or 64 lanes, the same bits in every lane: within 16
-// lanes by lane permutations in the add itself (xor 1, xor 2, mirrored halves,
-// mirrored rows), beyond by exchanging rows and halves.
+// Sum over groups of L = 4, 8, 16, 32 or 64 lanes, the same bits in every lane:
+// within 16 lanes by lane permutations in the add itself (xor 1, xor 2, mirrored
+// halves, mirrored rows), beyond by exchanging rows and halves.
 template <int CTRL>
 __device__ __forceinline__ float dpp(float v) {
   return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), CTRL, 0xf, 0xf, true));
@@ -124,13 +124,13 @@ template <int L>
 __device__ __forceinline__ float lane_sum(float v) {
   v += dpp<0xb1>(v);
   v += dpp<0x4e>(v);
-  if constexpr (L >= 16) {
-    v += dpp<0x141>(v);
-    v += dpp<0x140>(v);
-  }
-  if constexpr (L == 64) {
+  if constexpr (L >= 8) v += dpp<0x141>(v);
+  if constexpr (L >= 16) v += dpp<0x140>(v);
+  if constexpr (L >= 32) {
     auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  }
+  if constexpr (L >= 64) {
     auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     v = __uint_as_float(b[0]) + __uint_as_float(b[1]);
   }
@@ -316,8 +316,8 @@ hipError_t launch_rope(int bf16, const RopeArgs& args, hipStream_t s) {
 // ---------------------------------------------------------------------------
 // layer norm
 // ---------------------------------------------------------------------------
-// Layouts of the row kernels: a row is held by `lanes` threads (4 or 16 of a wave,
-// a wave, or W waves), K chunks of 16 bytes each; a workgroup of the forward takes
+// Layouts of the row kernels: a row is held by `lanes` threads (4 to 64 of a wave,
+// or W waves), K chunks of 16 bytes each; a workgroup of the forward takes
 // `groups` rows, one of the backward as many as 1024 threads hold.
 template <typename E, int Lanes, int Waves, int Chunks, bool Narrow = false>
 struct RowShape {
@@ -333,7 +333,8 @@ namespace {
 
 // Calls f with the shape that holds a row of `cols` elements in the forward, and
 // in the backward (whose workgroups have 1024 threads).  Narrow rows share a wave
-// (1196284 x 26 bf16: 32 us with 4 lanes a row, 89 with 16).  The forward takes the
+// (1196284 x 26 bf16: 32 us with 4 lanes a row, 89 with 16; 161542 x 201: 34 with 32,
+// 57 with 64).  The forward takes the
 // fewest waves that hold the row with weight and bias: rows of a wave need no
 // barrier (16000 x 1500: 21.5 us with 3 chunks a lane, 25.6 with 4 waves), and
 // several rows of a compute unit are in flight (3605 x 4160: 17.3 us with 4 waves
@@ -344,7 +345,9 @@ auto with_norm_shape(int cols, F&& f) {
   constexpr int V = Chunk<T>::V;
   if (cols < V) return f(RowShape<T, 4, 1, 1, true>());
   if (cols <= 4 * V) return f(RowShape<T, 4, 1, 1>());
+  if (cols <= 8 * V) return f(RowShape<T, 8, 1, 1>());
   if (cols <= 16 * V) return f(RowShape<T, 16, 1, 1>());
+  if (cols <= 32 * V) return f(RowShape<T, 32, 1, 1>());
   if (cols <= 64 * V) return f(RowShape<T, 64, 1, 1>());
   if (cols <= 128 * V) return f(RowShape<T, 64, 1, 2>());
   if (cols <= 192 * V) return f(RowShape<T, 64, 1, 3>());
@@ -361,7 +364,9 @@ auto with_norm_bwd_shape(int cols, F&& f) {
   constexpr int V = Chunk<T>::V;
   if (cols < V) return f(RowShape<T, 4, 1, 1, true>());
   if (cols <= 4 * V) return f(RowShape<T, 4, 1, 1>());
+  if (cols <= 8 * V) return f(RowShape<T, 8, 1, 1>());
   if (cols <= 16 * V) return f(RowShape<T, 16, 1, 1>());
+  if (cols <= 32 * V) return f(RowShape<T, 32, 1, 1>());
   if (cols <= 64 * V) return f(RowShape<T, 64, 1, 1>());
   if (cols <= 128 * V) return f(RowShape<T, 64, 2, 1>());
   if (cols <= 256 * V) return f(RowShape<T, 64, 4, 1>());
