@@ -167,6 +167,31 @@ def test_rope_of_a_packed_projection_and_of_nothing():
         assert qo.shape == e.shape and ko.shape == e.shape
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("D,rot", [(64, 64), (48, 20), (27, 6), (80, 34)])
+def test_rope_mixed_places_and_layouts(dtype, layout, D, rot):
+    """q written elsewhere in another order of dimensions while k stays in place,
+    and the other way round; more key heads than query heads."""
+    import torch
+    rng = np.random.Generator(np.random.PCG64(D + rot))
+    B, T, Hq, Hk = 3, 19, 2, 5
+    spec, pos = dict(rot_dim=rot), np.arange(T)[None].repeat(B, 0) + 7
+    table = ops.rope_table(rot)
+    for q_in_place in (False, True):
+        q, qr = _dev(rng.normal(size=(B, T, Hq, D)), dtype)
+        k, kr = _dev(rng.normal(size=(B, T, Hk, D)), dtype)
+        other = lambda x: torch.full((x.shape[0], x.shape[2], x.shape[1], D + 1), 7.0, dtype=x.dtype, device="cuda")
+        buf = other(k if q_in_place else q)  # [B][H][T][D + 1]
+        away = buf[..., :D].transpose(1, 2)
+        out = (q, away) if q_in_place else (away, k)
+        ops.rope(q, k, table, start=7, layout=layout, out=out)
+        torch.cuda.synchronize()
+        _check_rope(_np(out[0]), qr, pos, spec, layout, 1.0, dtype, (D, rot, q_in_place, "q"))
+        _check_rope(_np(out[1]), kr, pos, spec, layout, 1.0, dtype, (D, rot, q_in_place, "k"))
+        assert bool((buf[..., D] == 7.0).all())
+
+
 def test_rope_positions_of_long_rows():
     """Rows of positions 200000 apart, and a single row whose stride says nothing."""
     import torch
@@ -472,6 +497,61 @@ def test_dropout_counters(seed, offset, step):
         assert np.array_equal(_np(got) > 0, oo.dropout_kept(3, 50, 0.5, seed, (offset + step) % (1 << 64))[0])
         return
     _drop_case("f32", 6, 100, 0.5, seed, offset, step=step)
+
+
+def _loose(rng, R, C, dtype, values=None):
+    """A [R][C] tensor at an address and a pitch of its own: (view, buffer, lead, pitch, float64 values)."""
+    import torch
+    lead, ld = int(rng.integers(0, 9)), C + int(rng.integers(0, 12))
+    t, ref = _dev(rng.normal(size=(R, C)) if values is None else values, dtype)
+    v, buf = _inside(t, lead, ld)
+    return v, buf, lead, ld, ref
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_every_operand_at_a_place_of_its_own(seed):
+    import torch
+    rng = np.random.Generator(np.random.PCG64(1000 + seed))
+    dtype = ["bf16", "f32"][seed % 2]
+    R, C = int(rng.integers(1, 200)), int(np.exp(rng.uniform(0, np.log(5000))))
+    print("[places]", seed, dtype, R, C, flush=True)
+    bufs = []
+
+    def loose(values=None):
+        v, buf, lead, ld, ref = _loose(rng, R, C, dtype, values)
+        bufs.append((buf, lead, ld))
+        return v, ref
+
+    x, xr = loose(rng.normal(size=(R, C)) + 1)
+    res, rr = loose()
+    dy, dr = loose()
+    y, _ = loose()
+    dx, _ = loose()
+    z, _ = loose()
+    off = int(rng.integers(0, 4))
+    vec = lambda: torch.from_numpy(rng.normal(size=C + off).astype(np.float32)).cuda()[off:]
+    w, b = vec(), vec()
+    _, m, r = ops.layer_norm(x, w, b, out=(y, torch.empty(R, device="cuda"), torch.empty(R, device="cuda")))
+    got = ops.layer_norm_backward(dy, x, w, m, r, residual=res, out=(dx, vec(), vec()))
+    ops.dropout(x, 0.3, seed, 5, residual=res, out=z)
+    torch.cuda.synchronize()
+    want, wm, wr = oo.layer_norm(xr, _np(w), _np(b))
+    by = _norm_bounds(xr, _np(w), _np(b), wm, wr, want, dtype, C, 1e-5)[0]
+    assert (np.abs(_np(y) - want) - by).max() <= TINY
+    d64 = oo.layer_norm_backward(dr, xr, _np(w), _np(m), _np(r), rr)
+    h = np.abs(xr - _np(m)[:, None]) * _np(r)[:, None]
+    g = np.abs(dr * _np(w))
+    n = C + 2
+    # as in _norm_bwd_case, with |mean(g h)| bounded by the mean of |g h|
+    inner = g * 4 * U + (g.mean(1) * (n + 5) * U)[:, None] + h * ((g * h).mean(1) * (n + 11) * U)[:, None]
+    bx = _np(r)[:, None] * inner * 1.01 + 2 * U * np.abs(rr) + (HALF[dtype] + U) * np.abs(d64[0])
+    assert (np.abs(_np(dx) - d64[0]) - bx).max() <= TINY
+    assert (np.abs(_np(got[1]) - d64[1]) - (R + 4) * U * (np.abs(dr) * h).sum(0)).max() <= TINY
+    assert (np.abs(_np(got[2]) - d64[2]) - (R + 1) * U * np.abs(dr).sum(0)).max() <= TINY
+    drop = oo.dropout(xr, 0.3, seed, 5, rr)
+    assert (np.abs(_np(z) - drop) - 3 * U * np.abs(xr) * 1.5 - (U + HALF[dtype]) * np.abs(drop)).max() <= TINY
+    for buf, lead, ld in bufs:
+        assert _rest_untouched(buf, lead, R, C, ld)
 
 
 def test_dropped_elements_contribute_nothing():

@@ -89,6 +89,43 @@ def test_a_rotation_by_no_angle_changes_nothing():
     _bits_equal(plain, same)
 
 
+def test_without_kept_gradients_and_beside_another_context():
+    """No gradient buffers, and a plain trainer stepping in between: same numbers."""
+    cfg = synth_tf.tf_config("tf_small", **ALL)
+    params, batches = synth_tf.make_workload(cfg, seed=10, n_batches=2)
+    _, want = _gpu_run(cfg, params, batches)
+    plain = synth_tf.tf_config("tf_small")
+    pp, pb = synth_tf.make_workload(plain, seed=11, n_batches=1)
+    other = _trainer(plain, pp)
+    tr = _trainer(cfg, params, keep_grads=False)
+    for tok in batches:
+        t, o = tr.device_tokens(tok), other.device_tokens(pb[0])
+        tr.step(t, "overlap")
+        other.step(o, "overlap")
+    tr.sync()
+    other.sync()
+    p, m, v, g = tr.flat_state()
+    assert all(x is None for x in g)
+    for got, ref in ((p, want[-1]["params"]), (m, want[-1]["m"]), (v, want[-1]["v"])):
+        assert all(np.array_equal(a, b) for a, b in zip(got, ref))
+    tr.close()
+    other.close()
+
+
+def test_a_token_out_of_range_is_reported():
+    from paper_2608_18469_amd import erase
+    cfg = synth_tf.tf_config("tf_tiny", **ALL)
+    params, batches = synth_tf.make_workload(cfg, seed=12, n_batches=1)
+    tok = batches[0].copy()
+    tok[0, 3] = cfg["vocab"]
+    tr = _trainer(cfg, params)
+    tr.step(tr.device_tokens(tok), "serial")
+    with pytest.raises(erase.EraseError) as e:
+        tr.sync()
+    assert e.value.status == erase.ERR_INVALID_ARG
+    tr.close()
+
+
 def test_timing_records_with_options():
     cfg = synth_tf.tf_config("tf_small", **ALL)
     params, batches = synth_tf.make_workload(cfg, seed=9, n_batches=1)
