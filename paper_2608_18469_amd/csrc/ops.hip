@@ -16,13 +16,16 @@ namespace erase {
 
 namespace {
 
-// hipLaunchKernel's own result (not the last error of any earlier call).
+// hipLaunchKernel's own result (not the last error of any earlier call, and none
+// left behind for a later one).
 template <typename A>
 hipError_t launch1(void (*kernel)(A), int64_t grid, int block, const A& a, hipStream_t s, uint32_t grid_y = 1) {
   A copy = a;
   void* args[] = {&copy};
-  return hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3((uint32_t)grid, grid_y), dim3((uint32_t)block), args,
-                         0, s);
+  const hipError_t e = hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3((uint32_t)grid, grid_y),
+                                       dim3((uint32_t)block), args, 0, s);
+  if (e != hipSuccess) (void)hipGetLastError();
+  return e;
 }
 
 // Eight bf16 or four fp32 consecutive elements, moved by one 16-byte access from
@@ -334,12 +337,11 @@ namespace {
 // Calls f with the shape that holds a row of `cols` elements in the forward, and
 // in the backward (whose workgroups have 1024 threads).  Narrow rows share a wave
 // (1196284 x 26 bf16: 32 us with 4 lanes a row, 89 with 16; 161542 x 201: 34 with 32,
-// 57 with 64).  The forward takes the
-// fewest waves that hold the row with weight and bias: rows of a wave need no
-// barrier (16000 x 1500: 21.5 us with 3 chunks a lane, 25.6 with 4 waves), and
-// several rows of a compute unit are in flight (3605 x 4160: 17.3 us with 4 waves
-// of 3 chunks, 25.5 with 16 of 1).  The backward holds three times as much a
-// column and takes one chunk a lane while it can.
+// 57 with 64).  The forward takes the fewest waves that hold the row with weight
+// and bias: rows of a wave need no barrier (16000 x 1500: 21.5 us with 3 chunks a
+// lane, 25.6 with 4 waves), and several rows of a compute unit are in flight (3605
+// x 4160: 17.3 us with 4 waves of 3 chunks, 25.5 with 16 of 1).  The backward holds
+// three times as much a column and takes one chunk a lane while it can.
 template <typename T, typename F>
 auto with_norm_shape(int cols, F&& f) {
   constexpr int V = Chunk<T>::V;
@@ -568,7 +570,7 @@ hipError_t launch_norm(int bf16, const NormArgs& a, hipStream_t s) {
     if (!bf16 || a.cols % 64 || a.cols > 4096) return hipErrorInvalidValue;
     auto run = [&](auto sh) {
       typedef decltype(sh) S;
-      if constexpr (!S::narrow && S::cols <= 4096) return launch1(ops_norm<S, true>, grid(sh), sh.threads, a, s);
+      if constexpr (S::cols >= 64 && S::cols <= 4096) return launch1(ops_norm<S, true>, grid(sh), sh.threads, a, s);
       return hipErrorInvalidValue;
     };
     return with_norm_shape<uint16_t>(a.cols, run);
@@ -864,7 +866,7 @@ hipError_t launch_norm_bwd(int bf16, const NormBwdArgs& args, hipStream_t s) {
     if (!bf16 || a.cols % 64 || a.cols > 4096 || a.strips) return hipErrorInvalidValue;
     auto run = [&](auto sh) {
       typedef decltype(sh) S;
-      if constexpr (!S::narrow && S::cols <= 4096)
+      if constexpr (S::cols >= 64 && S::cols <= 4096)
         return launch1(a.dyscale ? ops_norm_bwd<S, HEAD> : ops_norm_bwd<S, F32>, a.nparts, 1024, a, s);
       return hipErrorInvalidValue;
     };
