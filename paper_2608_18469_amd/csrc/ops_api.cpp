@@ -119,7 +119,8 @@ erase_status rope(const erase_rope_config* cfg, const void* q, const void* k, vo
   if (!q || !qo || misaligned(q, es) || misaligned(qo, es) || !table || misaligned(table, 8) ||
       misaligned(positions, 4))
     return ERASE_ERR_INVALID_ARG;
-  if (c.k_heads > 0 && (!k || !ko || misaligned(k, es) || misaligned(ko, es))) return ERASE_ERR_INVALID_ARG;
+  if (c.k_heads > 0 && (!k || !ko || misaligned(k, es) || misaligned(ko, es) || qo == ko || qo == k || ko == q))
+    return ERASE_ERR_INVALID_ARG;
   auto in_place = [](const void* x, const void* y, const int64_t n[3], const int64_t xs[3], const int64_t ys[3]) {
     if (x != y) return true;
     for (int d = 0; d < 3; ++d)
@@ -261,7 +262,8 @@ erase_status erase_layer_norm(const erase_norm_config* cfg, const void* x, const
   if (misaligned(w, 4) || misaligned(b, 4) || misaligned(mean, 4) || misaligned(rstd, 4)) return ERASE_ERR_INVALID_ARG;
   if (c.rows == 0) return ERASE_OK;
   const size_t es = elem(c.dtype);
-  if (!x || !y || misaligned(x, es) || misaligned(y, es) || !same_or_apart(y, c.y_ld, x, c.x_ld, c.rows))
+  if (!x || !y || misaligned(x, es) || misaligned(y, es) || !same_or_apart(y, c.y_ld, x, c.x_ld, c.rows) ||
+      (mean && mean == rstd))
     return ERASE_ERR_INVALID_ARG;
   NormArgs a{};
   a.x = x;

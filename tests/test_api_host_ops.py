@@ -99,6 +99,14 @@ def test_rope_refusals(fn, kw, code):
     assert _rope(fn, **kw) == code
 
 
+@pytest.mark.parametrize("fn", ["erase_rope", "erase_rope_backward"])
+def test_rope_outputs_in_one_place(fn):
+    same = (768, 256, 64)
+    for kw in (dict(ko=R), dict(q=P, k=P, qo=P, ko=P, k_heads=4), dict(qo=Q), dict(ko=P)):
+        assert _rope(fn, k_stride=same, ko_stride=same, **kw) == INVALID, kw
+    assert _rope(fn, ko=R, batch=0) == erase.OK  # (nothing is written)
+
+
 def test_rope_of_nothing():
     assert _rope(batch=0, q=None, k=None, qo=None, ko=None, table=None) == erase.OK
     assert _rope(seq=0, q=None, k=None, qo=None, ko=None, table=None) == erase.OK
@@ -110,6 +118,10 @@ def _norm(x=P, w=None, b=None, y=Q, mean=None, rstd=None, **kw):
     for name, v in kw.items():
         setattr(c, name, v)
     return ops.lib().erase_layer_norm(ctypes.byref(c), x, w, b, y, mean, rstd, None)
+
+
+def test_norm_statistics_in_one_place():
+    assert _norm(mean=R, rstd=R) == INVALID
 
 
 @pytest.mark.parametrize("kw,code", [
