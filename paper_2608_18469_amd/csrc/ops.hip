@@ -382,20 +382,21 @@ auto with_norm_bwd_shape(int cols, F&& f) {
 // The V columns that a thread's chunk i covers: [at, at + V), of which the first
 // `skip` belong to the chunk before.  A row's last chunk ends with the row, so
 // that every load is a whole one and none waits in a branch for the row's last
-// columns (0 to 7 of them); a thread behind the row skips all V.
+// columns (0 to 7 of them); a thread behind the row skips all V.  The first
+// `Whole` chunks are known to have nothing to skip.
 struct Window {
   int at, skip;
 };
-template <typename S>
+template <typename S, int Whole = 0>
 __device__ __forceinline__ Window window(int pos, int i, int cols) {
   constexpr int V = Chunk<typename S::T>::V;
   const int c = (pos + i * S::lanes) * V, at = min(c, cols - V);
-  return {at, min(c - at, V)};
+  return i < Whole ? Window{c, 0} : Window{at, min(c - at, V)};
 }
 // Chunk i of every thread lies within the row: nothing to skip.
-template <typename S>
+template <typename S, int Whole = 0>
 __device__ __forceinline__ bool whole(int i, int cols) {
-  return (i + 1) * S::lanes * Chunk<typename S::T>::V <= cols;
+  return i < Whole || (i + 1) * S::lanes * Chunk<typename S::T>::V <= cols;
 }
 // The V elements of a window (rows narrower than V: one by one).
 template <typename S, typename T>
@@ -725,41 +726,58 @@ __device__ __forceinline__ void norm_strip(const NormBwdArgs& a, int strip, floa
 }  // namespace
 
 // Backward.  A thread keeps its columns' weights and its partial sums of dw and
-// db in registers over all its rows.  At the end the workgroup's row groups are
-// added in order through LDS and one partial row per workgroup is stored (a
-// single workgroup stores dw and db themselves).  Workgroups of 1024 threads, one
-// a compute unit, keep the partial rows few: 16384 x 512 bf16 with res takes 16.1
-// us and the launch that adds them up 3.9 (in all 23 with 512 of 256 threads, 31
-// with 256 of 256: too few rows in flight).  16384 x 4096 takes 79.6 and 4.9 us,
-// 5.1 TB/s.  The next row's loads are issued ahead where a row's
-// waves meet at a barrier (17495 x 1083: 42.9 us, 47.0 without; rows of one wave
-// lose up to a tenth by it).
+// db in registers over all its rows.  With 16 columns a thread (rows of more than
+// 8192) the sums stand in LDS, in places that no other thread uses, since all of
+// it spills in registers: 2500 x 16384 bf16 with res takes 86 us (117 with spills,
+// 93 with the weights in LDS, 88 with the next row loaded ahead as well), fp32 148
+// (189, 160, 164).  At the end the workgroup's row groups are added in order
+// through LDS and one partial row per workgroup is stored (a single workgroup
+// stores dw and db themselves).  Workgroups of 1024 threads, one a compute unit,
+// keep the partial rows few: 16384 x 512 bf16 with res takes 16.1 us and the launch
+// that adds them up 3.9 (in all 23 with 512 of 256 threads, 31 with 256 of 256: too
+// few rows in flight).  16384 x 4096 takes 79.6 and 4.9 us, 5.1 TB/s.  The next
+// row's loads are issued ahead where a row's waves meet at a barrier (17495 x 1083:
+// 42.9 us, 47.0 without; rows of one wave lose up to a tenth by it).
 template <typename S, NormMode M>
 __global__ __launch_bounds__(1024) void ops_norm_bwd(NormBwdArgs a) {
   typedef typename S::T T;
   constexpr int V = Chunk<T>::V, G = S::bwd_groups, L = S::L, W = S::W, K = S::K;
   __shared__ float2 sums[2][G][W];
-  __shared__ float comb[G > 1 ? G * S::cols : M == PLAIN ? 1024 * V : 1];
+  constexpr bool kFew = K * V <= 8;  // elements a thread holds
+  // the row groups' sums at the end, or (not few) every thread's own sums
+  constexpr int kSums = !kFew ? 2 * S::cols : G > 1 ? G * S::cols : M == PLAIN ? 1024 * V : 4;
+  __shared__ float4 lds[kSums / 4];
+  float* comb = reinterpret_cast<float*>(lds);
   if constexpr (M == PLAIN)
     if ((int)blockIdx.x >= a.nparts) {
       norm_strip<S>(a, (int)blockIdx.x - a.nparts, comb);
       return;
     }
-  const int grp = threadIdx.x / S::lanes, pos = threadIdx.x % S::lanes;
-  float w[K][V], aw[K][V], ab[K][V];
+  // (a wave's one row group in a scalar register: so are its rows' addresses and
+  // statistics; 17495 x 1083: 49.4 us, 50.8 without)
+  const int grp = L == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x / S::lanes) : threadIdx.x / S::lanes;
+  const int pos = threadIdx.x % S::lanes;
+  constexpr int H = K / 2;  // chunks that are whole: else a shape of fewer is taken
+  float w[K][V], aw[kFew ? K : 1][V], ab[kFew ? K : 1][V];
   Window at[K];
 #pragma unroll
   for (int i = 0; i < K; ++i) {
-    at[i] = window<S>(pos, i, a.cols);
+    at[i] = window<S, H>(pos, i, a.cols);
     ld_weights<S>(a.w, at[i], 1.f, w[i]);
 #pragma unroll
-    for (int k = 0; k < V; ++k) aw[i][k] = ab[i][k] = 0.f;
+    for (int k = 0; k < V; ++k) {
+      if constexpr (kFew)
+        aw[i][k] = ab[i][k] = 0.f;
+      else if (k % 4 == 0)
+        lds[(i * V + k) / 4 * 2048 + threadIdx.x] = lds[(i * V + k) / 4 * 2048 + 1024 + threadIdx.x] =
+            make_float4(0.f, 0.f, 0.f, 0.f);
+    }
   }
   const float inv = 1.f / (float)a.cols;
   int buf = 0;
   const int64_t first = (int64_t)blockIdx.x * G;
   NormRow<S, M> cur, next;
-  constexpr bool kFew = K * V <= 8, kAhead = W > 1 && kFew;  // elements a thread holds
+  constexpr bool kAhead = W > 1 && kFew;
   if constexpr (kAhead) next = ld_norm_row<S, M>(a, at, first + grp < a.rows ? first + grp : first);
   // the same number of rounds for every row group of the workgroup
   for (int64_t n0 = first; n0 < a.rows; n0 += (int64_t)a.nparts * G) {
@@ -777,7 +795,7 @@ __global__ __launch_bounds__(1024) void ops_norm_bwd(NormBwdArgs a) {
     // what is not the thread's adds nothing: columns of the chunk before, rows behind the last
 #pragma unroll
     for (int i = 0; i < K; ++i)
-      if (!whole<S>(i, a.cols)) {
+      if (!whole<S, H>(i, a.cols)) {
         clear_front(x[i], at[i].skip);
         clear_front(d[i], at[i].skip);
       }
@@ -787,21 +805,38 @@ __global__ __launch_bounds__(1024) void ops_norm_bwd(NormBwdArgs a) {
     }
     float sg = 0.f, sgh = 0.f;
 #pragma unroll
-    for (int i = 0; i < K; ++i)
+    for (int i = 0; i < K; ++i) {
+      float h[V];
 #pragma unroll
       for (int k = 0; k < V; ++k) {
-        const float dv = d[i][k], h = (x[i][k] - mean) * r, g = dv * w[i][k];
+        const float dv = d[i][k], g = dv * w[i][k];
+        h[k] = (x[i][k] - mean) * r;
         sg += g;
-        sgh = fmaf(g, h, sgh);
-        aw[i][k] = fmaf(dv, h, aw[i][k]);
-        ab[i][k] += dv;
+        sgh = fmaf(g, h[k], sgh);
+        if constexpr (kFew) {
+          aw[i][k] = fmaf(dv, h[k], aw[i][k]);
+          ab[i][k] += dv;
+        }
       }
+      if constexpr (!kFew) {
+#pragma unroll
+        for (int k = 0; k < V; k += 4) {
+          float4 *p = lds + (i * V + k) / 4 * 2048 + threadIdx.x, *q = p + 1024, sw = *p, sb = *q;
+          sw.x = fmaf(d[i][k], h[k], sw.x), sb.x += d[i][k];
+          sw.y = fmaf(d[i][k + 1], h[k + 1], sw.y), sb.y += d[i][k + 1];
+          sw.z = fmaf(d[i][k + 2], h[k + 2], sw.z), sb.z += d[i][k + 2];
+          sw.w = fmaf(d[i][k + 3], h[k + 3], sw.w), sb.w += d[i][k + 3];
+          *p = sw;
+          *q = sb;
+        }
+      }
+    }
     if (M == F32 ? !a.dx32 : !a.dx) continue;
-    Chunk<T> res[K];  // asked for before the sums are known, where registers allow
+    Chunk<T> res[K];  // asked for before the sums are known
 #pragma unroll
     for (int i = 0; i < K; ++i) {
       res[i].r = u32x4_t{0u, 0u, 0u, 0u};
-      if (kFew && a.res) res[i] = ld_window<S>(static_cast<const T*>(a.res) + n * a.ldres, at[i]);
+      if (a.res) res[i] = ld_window<S>(static_cast<const T*>(a.res) + n * a.ldres, at[i]);
     }
     sg = lane_sum<L>(sg);
     sgh = lane_sum<L>(sgh);
@@ -823,7 +858,6 @@ __global__ __launch_bounds__(1024) void ops_norm_bwd(NormBwdArgs a) {
       // g and h are unpacked again: held over the reduction they cost 2 K V registers
       asm volatile("" : "+v"(x[i].r));
       if constexpr (M != HEAD) asm volatile("" : "+v"(d[i].r));
-      if (!kFew && a.res) res[i] = ld_window<S>(static_cast<const T*>(a.res) + n * a.ldres, at[i]);
       float o[V];
 #pragma unroll
       for (int k = 0; k < V; ++k) o[k] = fmaf(r, d[i][k] * w[i][k] - mg - (x[i][k] - mean) * r * mgh, res[i][k]);
@@ -840,9 +874,22 @@ __global__ __launch_bounds__(1024) void ops_norm_bwd(NormBwdArgs a) {
   if (!a.part) return;
   const bool alone = a.nparts == 1;
   float* part = a.part + (int64_t)blockIdx.x * 2 * a.ldpart;
-  st_norm_part<S>(aw, at, comb, grp, a.cols, alone ? a.dw : part);
-  if constexpr (G > 1) __syncthreads();
-  st_norm_part<S>(ab, at, comb, grp, a.cols, alone ? a.db : part + a.ldpart);
+  if constexpr (kFew) {
+    st_norm_part<S>(aw, at, comb, grp, a.cols, alone ? a.dw : part);
+    if constexpr (G > 1) __syncthreads();
+    st_norm_part<S>(ab, at, comb, grp, a.cols, alone ? a.db : part + a.ldpart);
+  } else {
+    for (int which = 0; which < 2; ++which) {
+      float* to = alone ? (which ? a.db : a.dw) : part + which * a.ldpart;
+      if (!to) continue;
+#pragma unroll
+      for (int i = 0; i < K; ++i)
+#pragma unroll
+        for (int k = 0; k < V; ++k)
+          if (k >= at[i].skip)
+            to[at[i].at + k] = comb[(((i * V + k) / 4 * 2 + which) * 1024 + (int)threadIdx.x) * 4 + k % 4];
+    }
+  }
 }
 
 // Partial rows: one per workgroup, a workgroup per compute unit; a single one

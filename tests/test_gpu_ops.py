@@ -410,6 +410,15 @@ def test_layer_norm_backward_around_one_launch(dtype, R, C):
     _norm_bwd_case(dtype, R, C, alias="dy")
 
 
+@pytest.mark.parametrize("R", [2, 770, 1029])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("C", [8193, 12345, 16384])
+def test_layer_norm_backward_of_the_widest_rows(dtype, C, R):
+    """Sums of columns in one workgroup's rounds of rows, in uneven numbers."""
+    _norm_bwd_case(dtype, R, C, res=R % 2 == 0, gap=C % 2)
+    _norm_bwd_case(dtype, R, C, weight=False, need=(R % 2 == 0, True, R % 2 == 1))
+
+
 @pytest.mark.parametrize("need", [(True, False, False), (False, True, False), (False, False, True), (True, True, False),
                                   (False, True, True), (True, False, True), (False, False, False)])
 @pytest.mark.parametrize("R", [0, 7, 600])
