@@ -187,9 +187,13 @@ def rope_table(rot_dim, base=10000.0, scaling="none", factor=1.0, original_lengt
     spec = _rope_spec(rot_dim, base, scaling, factor, original_length, fast, slow)
     n = c_size_t(0)
     _check(lib().erase_rope_table_bytes(ctypes.byref(spec), ctypes.byref(n)), "erase_rope_table_bytes")
+    dev = None if device is None else torch.device(device)
+    if dev is not None and dev.type != "cuda":  # the fill would write to a host address
+        raise EraseError(ERR_INVALID_ARG, "erase_rope_table", "device must be a GPU")
     if not torch.cuda.is_available():
         raise RuntimeError("no HIP device available: the operators run only on the GPU")
-    dev = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
+    if dev is None:
+        dev = torch.device("cuda", torch.cuda.current_device())
     data = _empty(n.value // 8, torch.int64, dev, stream)
     _run("erase_rope_table", lib().erase_rope_table, data.get_device(), stream, ctypes.byref(spec), data.data_ptr())
     return RopeTable(spec, data)
