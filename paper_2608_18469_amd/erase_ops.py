@@ -177,6 +177,8 @@ class RopeTable:
     """A device table of erase_rope_table: read only, for any number of calls."""
 
     def __init__(self, spec: RopeSpec, data):
+        if data.dtype != torch.int64 or data.numel() < spec.rot_dim // 2 + 1 or not data.is_contiguous():
+            raise EraseError(ERR_INVALID_ARG, "RopeTable", "data must be rot_dim / 2 + 1 contiguous int64")
         self.rot_dim, self.data = spec.rot_dim, data
 
 

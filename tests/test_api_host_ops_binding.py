@@ -13,3 +13,16 @@ def test_a_table_lives_on_a_gpu(device):
     with pytest.raises(erase.EraseError) as e:
         ops.rope_table(64, device=device)
     assert e.value.status == INVALID
+
+
+def test_a_table_holds_its_pairs():
+    """Memory that is shorter than its rotation, or of another kind: a call would
+    read behind it."""
+    spec = ops.RopeSpec(64, 0, 10000.0, 1.0, 0.0, 32.0, 1.0)
+    assert ops.RopeTable(spec, torch.zeros(33, dtype=torch.int64)).rot_dim == 64
+    for data in (torch.zeros(32, dtype=torch.int64), torch.zeros(0, dtype=torch.int64), torch.zeros(33, dtype=torch.int32),
+                 torch.zeros(33, dtype=torch.float64), torch.zeros(66, dtype=torch.int64)[::2],
+                 torch.zeros(1, dtype=torch.int64).expand(33)):
+        with pytest.raises(erase.EraseError) as e:
+            ops.RopeTable(spec, data)
+        assert e.value.status == INVALID
