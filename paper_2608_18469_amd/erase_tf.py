@@ -13,7 +13,7 @@ from ctypes import POINTER, c_double, c_float, c_int32, c_int64, c_size_t, c_uin
 import numpy as np
 
 from . import erase, erase_ops, synth_tf
-from .erase import BlockBuffers, EraseError, KernelTime, OK
+from .erase import ERR_INVALID_ARG, BlockBuffers, EraseError, KernelTime, OK
 
 TF_KERNEL_KINDS = {0: "prologue", 1: "fwd_gemm", 3: "wgrad_gemm", 4: "dgrad_gemm", 5: "adam", 6: "bwd_gemm", 7: "empty",
                    11: "embed", 12: "rms_fwd", 13: "rms_bwd", 14: "attn_fwd", 15: "attn_bwd", 16: "head_norm",
@@ -92,13 +92,22 @@ def native_options(cfg: dict) -> TfOptions | None:
     r, norm, p = cfg.get("rope"), cfg.get("norm", "rms"), cfg.get("dropout", 0.0)
     if r is None and norm == "rms" and p == 0.0:
         return None
-    o = TfOptions(rope=0 if r is None else 1, norm=NORMS[norm], norm_eps=cfg.get("norm_eps", 1e-5), dropout=p,
+    where = "erase_tf_options"
+
+    def number(name, value, names):
+        if value not in names:
+            raise EraseError(ERR_INVALID_ARG, where, f"{name} must be one of {sorted(names)}")
+        return names[value]
+
+    o = TfOptions(rope=0 if r is None else 1, norm=number("norm", norm, NORMS), norm_eps=cfg.get("norm_eps", 1e-5), dropout=p,
                   seed=cfg.get("dropout_seed", 0))
     if r is not None:
-        o.rope_layout = erase_ops.LAYOUTS[r.get("layout", "half")]
-        o.rope_spec = erase_ops.RopeSpec(r["rot_dim"], erase_ops.SCALINGS[r.get("scaling", "none")], r.get("base", 10000.0),
-                                         r.get("factor", 1.0), r.get("original_length", 0.0), r.get("fast", 32.0),
-                                         r.get("slow", 1.0))
+        if "rot_dim" not in r:
+            raise EraseError(ERR_INVALID_ARG, where, "rope must give rot_dim")
+        o.rope_layout = number("layout", r.get("layout", "half"), erase_ops.LAYOUTS)
+        o.rope_spec = erase_ops.RopeSpec(r["rot_dim"], number("scaling", r.get("scaling", "none"), erase_ops.SCALINGS),
+                                         r.get("base", 10000.0), r.get("factor", 1.0), r.get("original_length", 0.0),
+                                         r.get("fast", 32.0), r.get("slow", 1.0))
     return o
 
 

@@ -3,7 +3,7 @@ by itself, before any memory is read or any HIP call is made (no GPU needed)."""
 import pytest
 import torch
 
-from paper_2608_18469_amd import erase, erase_ops as ops
+from paper_2608_18469_amd import erase, erase_ops as ops, erase_tf, synth_tf
 
 INVALID, SHAPE = erase.ERR_INVALID_ARG, erase.ERR_SHAPE
 
@@ -25,4 +25,15 @@ def test_a_table_holds_its_pairs():
                  torch.zeros(1, dtype=torch.int64).expand(33)):
         with pytest.raises(erase.EraseError) as e:
             ops.RopeTable(spec, data)
+        assert e.value.status == INVALID
+
+
+@pytest.mark.parametrize("opts", [
+    dict(norm="batch"), dict(norm=None), dict(rope=dict(rot_dim=64, layout="both")), dict(rope=dict(rot_dim=64, scaling="cubic")),
+    dict(rope=dict()), dict(rope=dict(base=500000.0))])
+def test_unknown_names_of_step_options(opts):
+    cfg = synth_tf.tf_config("tf_tiny", **opts)
+    for call in (lambda: erase_tf.native_options(cfg), lambda: erase_tf.param_count(cfg, 0), lambda: erase_tf.workspace_bytes(cfg)):
+        with pytest.raises(erase.EraseError) as e:
+            call()
         assert e.value.status == INVALID
