@@ -162,13 +162,22 @@ def _empty(shape, dtype, device, stream):
 def _rope_spec(rot_dim, base, scaling, factor, original_length, fast, slow) -> RopeSpec:
     if scaling not in SCALINGS:
         raise EraseError(ERR_INVALID_ARG, "rope", f"scaling must be one of {sorted(SCALINGS)}")
-    return RopeSpec(rot_dim, SCALINGS[scaling], base, factor, original_length, fast, slow)
+    return spec_of("rope", rot_dim, SCALINGS[scaling], base, factor, original_length, fast, slow)
+
+
+def spec_of(where, rot_dim, scaling, base, factor, original_length, fast, slow) -> RopeSpec:
+    """An erase_rope_spec of numbers (its field would take rot_dim modulo 2^32)."""
+    if not -1 << 31 <= rot_dim < 1 << 31:
+        raise EraseError(ERR_SHAPE, where, "rot_dim must be even, 2..1024")
+    return RopeSpec(rot_dim, scaling, base, factor, original_length, fast, slow)
 
 
 def rope_frequencies(rot_dim, base=10000.0, scaling="none", factor=1.0, original_length=0.0, fast=32.0, slow=1.0):
     """(angles per position of the rot_dim / 2 pairs, amplitude) on the host (erase_rope_frequencies)."""
     spec = _rope_spec(rot_dim, base, scaling, factor, original_length, fast, slow)
-    freq, amp = (c_double * max(1, rot_dim // 2))(), c_double(0)
+    n, amp = c_size_t(0), c_double(0)
+    _check(lib().erase_rope_table_bytes(ctypes.byref(spec), ctypes.byref(n)), "erase_rope_frequencies")
+    freq = (c_double * (rot_dim // 2))()
     _check(lib().erase_rope_frequencies(ctypes.byref(spec), freq, ctypes.byref(amp)), "erase_rope_frequencies")
     return list(freq), amp.value
 

@@ -105,9 +105,9 @@ def native_options(cfg: dict) -> TfOptions | None:
         if "rot_dim" not in r:
             raise EraseError(ERR_INVALID_ARG, where, "rope must give rot_dim")
         o.rope_layout = number("layout", r.get("layout", "half"), erase_ops.LAYOUTS)
-        o.rope_spec = erase_ops.RopeSpec(r["rot_dim"], number("scaling", r.get("scaling", "none"), erase_ops.SCALINGS),
-                                         r.get("base", 10000.0), r.get("factor", 1.0), r.get("original_length", 0.0),
-                                         r.get("fast", 32.0), r.get("slow", 1.0))
+        o.rope_spec = erase_ops.spec_of(where, r["rot_dim"], number("scaling", r.get("scaling", "none"), erase_ops.SCALINGS),
+                                        r.get("base", 10000.0), r.get("factor", 1.0), r.get("original_length", 0.0),
+                                        r.get("fast", 32.0), r.get("slow", 1.0))
     return o
 
 

@@ -37,3 +37,13 @@ def test_unknown_names_of_step_options(opts):
         with pytest.raises(erase.EraseError) as e:
             call()
         assert e.value.status == INVALID
+
+
+@pytest.mark.parametrize("rot_dim", [(1 << 32) + 64, 1 << 31, (1 << 31) - 2, -(1 << 32) + 64, 1 << 64])
+def test_rotations_beyond_32_bits_are_not_taken_modulo(rot_dim):
+    for call in (lambda: ops.rope_table(rot_dim), lambda: ops.rope_frequencies(rot_dim),
+                 lambda: erase_tf.workspace_bytes(synth_tf.tf_config("tf_tiny", rope=dict(rot_dim=rot_dim)))):
+        with pytest.raises(erase.EraseError) as e:
+            call()
+        assert e.value.status == SHAPE
+
