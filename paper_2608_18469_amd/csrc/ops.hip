@@ -474,8 +474,15 @@ __device__ __forceinline__ void st_window(T* p, const Window& w, const float v[C
 
 constexpr int kNormGroups = 2048;  // workgroups of the forward, eight a compute unit
 
-// Forward: a row is read once into registers; the mean, then the variance of the
-// centred row, two reductions that wait for one another.  A workgroup takes many
+// Forward: a row is read once into registers; the mean, then the sums of the
+// centred row and of its squares, two reductions that wait for one another.  The
+// rounded mean m leaves c = mean(x - m), which is taken off the row and its square
+// off the mean of squares: rows of one value are centred to zero, and rows far from
+// zero are off by the rounding of c, not of m (700 columns of 30000.3: y was -0.53).
+// The second sum, its correction and r as one rsqrt (within 1 ulp, twice a correctly
+// rounded quotient's error) take what the quotients by cols and of the square root
+// took: 16384 x 512 8.7 us, 9.2 with a square root and a quotient for r, 9.6 with all
+// quotients.  A workgroup takes many
 // rows, so that weight and bias (twice the bytes of a bf16 row each) are read
 // once per thread, not per row: 8000 x 4096 bf16 takes 27.7 us (4.7 TB/s), 34.9
 // with weight and bias read again for every row.
@@ -484,9 +491,17 @@ template <typename S, bool HEAD>
 __global__ __launch_bounds__(S::threads) void ops_norm(NormArgs a) {
   typedef typename S::T T;
   constexpr int V = Chunk<T>::V, L = S::L, W = S::W, K = S::K;
-  __shared__ float sums[HEAD ? 3 : 2][S::groups][W];
+  __shared__ float sums[HEAD ? 2 : 1][S::groups][W];
+  __shared__ float2 sums2[S::groups][W];
   const int grp = threadIdx.x / S::lanes, pos = threadIdx.x % S::lanes;
-  const float cols = (float)a.cols;
+  const float cols = (float)a.cols, inv = 1.f / cols;
+  // v / cols, rounded once: with 1 / cols rounded, the remainder of v * inv (exact in
+  // an fma) corrects it to the nearest (Markstein 1990), so that equal numbers have
+  // their own mean
+  auto over_cols = [&](float v) {
+    const float q = v * inv;
+    return fmaf(fmaf(-q, cols, v), inv, q);
+  };
   float w[K][V], b[K][V];
   Window at[K];
 #pragma unroll
@@ -503,6 +518,20 @@ __global__ __launch_bounds__(S::threads) void ops_norm(NormArgs a) {
       v = 0.f;
 #pragma unroll
       for (int j = 0; j < W; ++j) v += sums[which][grp][j];
+    }
+    return v;
+  };
+  auto total2 = [&](float2 v) {
+    v = make_float2(lane_sum<L>(v.x), lane_sum<L>(v.y));
+    if constexpr (W > 1) {
+      if ((threadIdx.x & 63) == 0) sums2[grp][pos >> 6] = v;
+      __syncthreads();
+      v = make_float2(0.f, 0.f);
+#pragma unroll
+      for (int j = 0; j < W; ++j) {
+        v.x += sums2[grp][j].x;
+        v.y += sums2[grp][j].y;
+      }
     }
     return v;
   };
@@ -524,26 +553,34 @@ __global__ __launch_bounds__(S::threads) void ops_norm(NormArgs a) {
         for (int k = 0; k < V; ++k) s += k >= at[i].skip ? x[i][k] : 0.f;
       }
     }
-    // (divided: the product with a rounded 1 / cols would not give a constant row its own value)
-    const float mean = total(s, 0) / cols;
-    float q = 0.f;
+    s = total(s, 0);
+    const float mean = isinf(s) ? s : over_cols(s);
+    float2 dq = make_float2(0.f, 0.f);
 #pragma unroll
     for (int i = 0; i < K; ++i) {
       if (whole<S>(i, a.cols)) {
 #pragma unroll
-        for (int k = 0; k < V; ++k) q = fmaf(x[i][k] - mean, x[i][k] - mean, q);
+        for (int k = 0; k < V; ++k) {
+          const float d = x[i][k] - mean;
+          dq.x += d;
+          dq.y = fmaf(d, d, dq.y);
+        }
       } else {
 #pragma unroll
         for (int k = 0; k < V; ++k) {
           const float d = k >= at[i].skip ? x[i][k] - mean : 0.f;
-          q = fmaf(d, d, q);
+          dq.x += d;
+          dq.y = fmaf(d, d, dq.y);
         }
       }
     }
-    const float r = 1.f / sqrtf(total(q, 1) / cols + a.eps);
+    dq = total2(dq);
+    // (apart from the mean: mean + left rounds again)
+    const float left = over_cols(dq.x), v = fmaf(-left, left, dq.y * inv);
+    const float r = rsqrtf((v < 0.f ? 0.f : v) + a.eps);  // (a NaN stays one)
     if (!HEAD && !row) continue;
     if (row && pos == 0) {
-      if (a.mean) a.mean[n] = mean;
+      if (a.mean) a.mean[n] = isinf(mean) ? mean : mean + left;
       if (a.rstd) a.rstd[n] = r;
     }
     const int32_t target = HEAD ? a.target[n] : -1;
@@ -552,7 +589,7 @@ __global__ __launch_bounds__(S::threads) void ops_norm(NormArgs a) {
     for (int i = 0; i < K; ++i) {
       float o[V];
 #pragma unroll
-      for (int k = 0; k < V; ++k) o[k] = fmaf((x[i][k] - mean) * r, w[i][k], b[i][k]);
+      for (int k = 0; k < V; ++k) o[k] = fmaf((x[i][k] - mean - left) * r, w[i][k], b[i][k]);
       if (row) st_window(static_cast<T*>(a.y) + n * a.ldy, at[i], o);
       if constexpr (HEAD) {
         if (target >= 0) {  // (whole chunks: cols is a multiple of V)
@@ -563,7 +600,7 @@ __global__ __launch_bounds__(S::threads) void ops_norm(NormArgs a) {
       }
     }
     if constexpr (HEAD) {
-      logit = total(logit, 2);
+      logit = total(logit, 1);
       if (row && pos == 0) a.xref[n] = logit;
     }
   }
