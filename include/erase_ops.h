@@ -132,10 +132,10 @@ ERASE_API erase_status erase_layer_norm(const erase_norm_config* cfg, const void
  * res (the gradient that reaches x by another path, such as a residual's) may
  * be NULL, and so may dx, dw and db where they are not wanted; no rows give
  * dw = db = 0.  dx may be dy or res, with the same pitch.  dw and db are summed
- * in fp32 in an order that depends on the sizes alone: equal calls give equal
- * bits.  scratch: erase_layer_norm_backward_scratch_bytes() bytes of device
- * memory (16-byte aligned, any contents), its own for every call in flight;
- * not read where neither dw nor db is wanted. */
+ * in fp32 in an order that depends on the type, the sizes and whether dx is dy:
+ * equal calls give equal bits.  scratch: erase_layer_norm_backward_scratch_bytes()
+ * bytes of device memory (16-byte aligned, any contents), its own for every call
+ * in flight; not read where neither dw nor db is wanted. */
 ERASE_API erase_status erase_layer_norm_backward_scratch_bytes(const erase_norm_config* cfg, size_t* bytes);
 ERASE_API erase_status erase_layer_norm_backward(const erase_norm_config* cfg, const void* x, const void* dy,
                                                  const float* w, const float* mean, const float* rstd, const void* res,
