@@ -70,11 +70,13 @@ ERASE_API erase_status erase_rope_frequencies(const erase_rope_spec* spec, doubl
 /* The device table of a spec: per pair the turns of one position as a 64-bit
  * fraction of a full turn, f_i / (2 pi) modulo 1 in units of 2^-64, then the
  * amplitude.  The product position * fraction modulo 2^64 is the angle modulo
- * a turn, off by at most |position| 2^-65 turns, so that far positions are as
- * accurate as near ones (fp32 angles are off by 0.03 radians at position
- * 2^20).  erase_rope_table() fills `table` (8-byte aligned device memory of
- * erase_rope_table_bytes()) on `stream`; a table is read only afterwards and
- * serves any number of calls. */
+ * a turn.  The table puts it off by at most |position| 2^-63 turns (BY_PARTS with
+ * fast and slow close together: times fast / (fast - slow)), and the kernel drops
+ * what is below 2^-32 turns (1.5e-9 radians).  So every int32 position is as
+ * accurate as a near one; position 2^40 is off by up to 7.5e-7 radians (an fp32
+ * angle by 0.03 at 2^20 already).  erase_rope_table() fills `table` (8-byte aligned
+ * device memory of erase_rope_table_bytes()) on `stream`; a table is read only
+ * afterwards and serves any number of calls. */
 ERASE_API erase_status erase_rope_table_bytes(const erase_rope_spec* spec, size_t* bytes);
 ERASE_API erase_status erase_rope_table(const erase_rope_spec* spec, void* table, void* stream);
 

@@ -140,8 +140,8 @@ __device__ __forceinline__ float lane_sum(float v) {
   return v;
 }
 
-// sine and cosine of a 64-bit fraction of a turn: the quadrant from the top
-// bits, then the Taylor polynomials on [-pi/4, pi/4] (next terms 1.8e-9 and
+// sine and cosine of a 64-bit fraction of a turn (its low half, less than 1.5e-9
+// radians, is dropped): the quadrant from the top bits, then the Taylor polynomials on [-pi/4, pi/4] (next terms 1.8e-9 and
 // 1.2e-10, below a quarter of an fp32 rounding of 1)
 __device__ __forceinline__ void sincos_turn(uint64_t turn, float& s, float& c) {
   const uint32_t t = (uint32_t)(turn >> 32) + 0x20000000u;  // + 1/8: quadrants centred on multiples of 1/4

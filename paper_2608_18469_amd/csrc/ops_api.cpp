@@ -36,7 +36,7 @@ erase_status done(hipError_t e) { return e == hipSuccess ? ERASE_OK : ERASE_ERR_
 // ---------------------------------------------------------------------------
 // rotary positions
 // ---------------------------------------------------------------------------
-constexpr double kTau = 6.283185307179586476925286766559;
+constexpr long double kTau = 6.283185307179586476925286766559006L;
 
 erase_status check_spec(const erase_rope_spec* p) {
   if (!p) return ERASE_ERR_INVALID_ARG;
@@ -55,23 +55,23 @@ double amplitude_of(const erase_rope_spec& p) {
   return p.scaling == ERASE_ROPE_BY_PARTS ? 0.1 * std::log(p.factor) + 1.0 : 1.0;
 }
 
-double frequency(const erase_rope_spec& p, int i) {
-  const double r = p.rot_dim, s = p.factor;
-  double base = p.base;
+// f_i in 64 significant bits: a table's angles are products with positions, which
+// multiply its rounding (a double's reached 2^-57 turns a position).
+long double frequency(const erase_rope_spec& p, int i) {
+  const long double r = p.rot_dim, s = p.factor;
+  long double base = p.base;
   if (p.scaling == ERASE_ROPE_NTK && p.rot_dim > 2) base *= std::pow(s, r / (r - 2));  // one pair: f = 1 for any base
-  const double g = std::pow(base, -2.0 * i / r);
+  const long double g = std::pow(base, -2.0L * i / r);
   if (p.scaling == ERASE_ROPE_LINEAR) return g / s;
   if (p.scaling != ERASE_ROPE_BY_PARTS) return g;
-  const double turns = p.original_length * g / kTau;
-  const double keep = std::min(1.0, std::max(0.0, (turns - p.slow) / (p.fast - p.slow)));
-  return g * keep + g / s * (1.0 - keep);
+  const long double turns = p.original_length * g / kTau, ramp = (turns - p.slow) / ((long double)p.fast - p.slow);
+  const long double keep = std::min(1.0L, std::max(0.0L, ramp));
+  return g * (keep + (1.0L - keep) / s);
 }
 
-// f / (2 pi) modulo 1 as a 64-bit fraction.  The quotient is taken in 64
-// significant bits and f <= 1, so the result is within half a unit or so.
-uint64_t turn_fraction(double f) {
-  const long double t = static_cast<long double>(f) / 6.283185307179586476925286766559006L;
-  return static_cast<uint64_t>(std::floor(std::ldexp(t, 64) + 0.5L));
+// f / (2 pi) modulo 1 as a 64-bit fraction, to the nearest.
+uint64_t turn_fraction(long double f) {
+  return static_cast<uint64_t>(std::floor(std::ldexp(f / kTau, 64) + 0.5L));
 }
 
 // The elements of an output [n0][n1][n2][dim] do not coincide: sorted by
@@ -208,7 +208,7 @@ extern "C" {
 erase_status erase_rope_frequencies(const erase_rope_spec* spec, double* freq, double* amplitude) {
   if (erase_status st = check_spec(spec); st != ERASE_OK) return st;
   if (!freq || !amplitude) return ERASE_ERR_INVALID_ARG;
-  for (int i = 0; i < spec->rot_dim / 2; ++i) freq[i] = frequency(*spec, i);
+  for (int i = 0; i < spec->rot_dim / 2; ++i) freq[i] = static_cast<double>(frequency(*spec, i));
   *amplitude = amplitude_of(*spec);
   return ERASE_OK;
 }
