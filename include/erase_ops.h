@@ -75,8 +75,9 @@ ERASE_API erase_status erase_rope_frequencies(const erase_rope_spec* spec, doubl
  * what is below 2^-32 turns (1.5e-9 radians).  So every int32 position is as
  * accurate as a near one; position 2^40 is off by up to 7.5e-7 radians (an fp32
  * angle by 0.03 at 2^20 already).  erase_rope_table() fills `table` (8-byte aligned
- * device memory of erase_rope_table_bytes()) on `stream`; a table is read only
- * afterwards and serves any number of calls. */
+ * device memory of erase_rope_table_bytes()) on `stream`; afterwards a table is
+ * only read and serves any number of calls.  A caller orders another stream that
+ * uses it after this one: no call waits for it. */
 ERASE_API erase_status erase_rope_table_bytes(const erase_rope_spec* spec, size_t* bytes);
 ERASE_API erase_status erase_rope_table(const erase_rope_spec* spec, void* table, void* stream);
 

@@ -7,7 +7,8 @@ ABI; PyTorch provides device memory and streams.  There is no fallback and no
 autograd: the backward passes are calls of their own.  Each function enqueues
 on ``stream`` (a torch stream of the tensors' device; default: that device's
 current stream), returns without waiting, and allocates the outputs that
-``out`` does not give.
+``out`` does not give.  Inputs written on another stream, and outputs read on one,
+are ordered by the caller, as with torch's own operations.
 """
 from __future__ import annotations
 
@@ -194,7 +195,9 @@ class RopeTable:
 def rope_table(rot_dim, base=10000.0, scaling="none", factor=1.0, original_length=0.0, fast=32.0, slow=1.0, device=None,
                stream=None) -> RopeTable:
     """The table of a rotation (erase_rope_spec's fields) on `device` (default: the
-    current GPU), filled on `stream`; calls on another stream wait for it."""
+    current GPU), filled on `stream`.  As with any tensor, a caller who uses it on
+    another stream orders that stream after this one (by an event or a
+    synchronisation): the calls themselves do not wait."""
     spec = _rope_spec(rot_dim, base, scaling, factor, original_length, fast, slow)
     n = c_size_t(0)
     _check(lib().erase_rope_table_bytes(ctypes.byref(spec), ctypes.byref(n)), "erase_rope_table_bytes")

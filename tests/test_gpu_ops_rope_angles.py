@@ -78,3 +78,25 @@ def test_positions_of_every_distance(spec, layout, start):
     bound = amp * (np.abs(x1) + np.abs(x2)) * (10 * U + far) + TINY
     for got, want in ((y1, amp * (x1 * cs - x2 * sn)), (y2, amp * (x2 * cs + x1 * sn))):
         assert (np.abs(got - want) - bound - U * np.abs(want)).max() <= 0
+
+
+def test_a_table_filled_on_a_busy_stream():
+    """A stream that the caller orders after the filling one reads a filled table,
+    with no synchronisation of the host in between."""
+    import torch
+    x = torch.randn((2, 300, 4, 64), device="cuda")
+    want, _ = ops.rope(x, None, ops.rope_table(64, base=777.0))
+    fill, use = torch.cuda.Stream(), torch.cuda.Stream()
+    big = torch.randn((4096, 4096), device="cuda")
+    torch.cuda.synchronize()
+    got, tables = [], []
+    for _ in range(3):
+        with torch.cuda.stream(fill):
+            for _ in range(20):  # a few milliseconds before the fill
+                big @ big
+        table = ops.rope_table(64, base=777.0, stream=fill)
+        use.wait_stream(fill)
+        tables.append(table)  # (its memory is the filling stream's)
+        got.append(ops.rope(x, None, table, stream=use)[0])
+    torch.cuda.synchronize()
+    assert all(torch.equal(y, want) for y in got)
