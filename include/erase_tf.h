@@ -33,7 +33,10 @@
  *   n1 = ln(a0; g1, b1);  [q | k | v] = n1 Wqkv^T;  q, k turned by position t
  *   a1 = a0 + drop(o Wo^T);  n2 = ln(a1; g2, b2);  z = a1 + drop(gelu(n2 W1^T) W2^T)
  *   l_b from ln(z; g3, b3)
- * with the operators of erase_ops.h.
+ * with the operators of erase_ops.h.  With dropout a branch (o Wo^T, gelu(n2 W1^T)
+ * W2^T) and the gradient at it are stored in bf16 before the mask and the sum with
+ * the residual, which is rounded to bf16 again; without, the sum is formed in fp32
+ * in the product's epilogue and rounded once.
  */
 #ifndef ERASE_TF_H_
 #define ERASE_TF_H_
