@@ -10,7 +10,7 @@
 #include <type_traits>
 
 #include "device.h"
-#include "internal.h"
+#include "ops.h"
 
 namespace erase {
 
@@ -298,7 +298,9 @@ hipError_t launch_rope(int bf16, const RopeArgs& args, hipStream_t s) {
   // as many tokens as give every thread one unit, or two where that leaves fewer
   // threads without any (57274 tokens of 144 units: 107 us with three tokens in
   // two rounds, 129 to 137 with one token on 144 of 256 threads; more rounds hide
-  // less latency: tokens of 320 units 82 us in two rounds of one, 92 in five of four);
+  // less latency: tokens of 320 units 82 us in two rounds of one, 92 in five of four;
+  // the second round is taken where it uses at least a twentieth of the threads more:
+  // 100000 tokens of 24 units, 10 of them a round, 35.3 us, 21 in two rounds 36.3);
   // fewer where that leaves less than two workgroups a compute unit
   int best = 1;
   double used = 0.0;  // share of the threads' rounds

@@ -7,7 +7,7 @@
 #include <cstring>
 
 #include "erase_ops.h"
-#include "internal.h"
+#include "ops.h"
 
 namespace {
 

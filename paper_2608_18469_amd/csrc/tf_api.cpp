@@ -19,6 +19,7 @@
 
 #include "erase_tf.h"
 #include "internal.h"
+#include "ops.h"
 #include "wide_plan.h"
 
 namespace {
