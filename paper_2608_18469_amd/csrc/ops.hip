@@ -176,8 +176,7 @@ hipError_t launch_rope_fill(const RopeFillArgs& a, hipStream_t s) { return launc
 // their sines and cosines once into LDS, then its threads take units of those
 // tokens' heads, 32 bytes each: V pairs (two 16-byte chunks) or 2 V columns that
 // pass.  HBM bounds it: 671 MB read and written (32768 tokens of 40 heads of 128,
-// half of each turned) take 124 us, 5.4 TB/s (the rest of a copy's rate comes from
-// the cache).  Columns that pass in units of one
+// half of each turned) take 129 us, 5.2 TB/s.  Columns that pass in units of one
 // chunk, on a path of their own, took 163 us; several units' loads issued before
 // the sines 162 to 224 (the registers cost more waves than the loads hide).
 constexpr int kRopePairs = 2048;  // pairs of a workgroup's tokens (16 KB of LDS)
@@ -486,7 +485,7 @@ constexpr int kNormGroups = 2048;  // workgroups of the forward, eight a compute
 // took: 16384 x 512 8.7 us, 9.2 with a square root and a quotient for r, 9.6 with all
 // quotients.  A workgroup takes many
 // rows, so that weight and bias (twice the bytes of a bf16 row each) are read
-// once per thread, not per row: 8000 x 4096 bf16 takes 27.7 us (4.7 TB/s), 34.9
+// once per thread, not per row: 8000 x 4096 bf16 takes 27.4 us (4.7 TB/s), 34.9
 // with weight and bias read again for every row.
 // HEAD: also the target logit of the stored row.
 template <typename S, bool HEAD>
@@ -776,9 +775,9 @@ __device__ __forceinline__ void norm_strip(const NormBwdArgs& a, int strip, floa
 // (189, 160, 164).  At the end the workgroup's row groups are added in order
 // through LDS and one partial row per workgroup is stored (a single workgroup
 // stores dw and db themselves).  Workgroups of 1024 threads, one a compute unit,
-// keep the partial rows few: 16384 x 512 bf16 with res takes 16.1 us and the launch
+// keep the partial rows few: 16384 x 512 bf16 with res takes 16.8 us and the launch
 // that adds them up 3.9 (in all 23 with 512 of 256 threads, 31 with 256 of 256: too
-// few rows in flight).  16384 x 4096 takes 79.6 and 4.9 us, 5.1 TB/s.  The next
+// few rows in flight).  16384 x 4096 takes 79.9 and 4.9 us, 5.0 TB/s.  The next
 // row's loads are issued ahead where a row's waves meet at a barrier (17495 x 1083:
 // 42.9 us, 47.0 without; rows of one wave lose up to a tenth by it).
 template <typename S, NormMode M>
@@ -1044,7 +1043,7 @@ __device__ __forceinline__ void philox(uint32_t x[4], uint32_t k0, uint32_t k1) 
 // A thread takes eight columns of a row: one counter, one or two chunks.  The
 // ten rounds are 20 products of 32 x 32 bits, which issue at a quarter of the
 // rate of an addition: 16 bits an element (rather than 32) keep them below the
-// time HBM needs.  16384 x 4096 bf16 takes 45.5 us for 268 MB read and written.
+// time HBM needs.  16384 x 4096 bf16 takes 45.7 us for 268 MB read and written.
 struct DropPlan {
   DropArgs a;
   FastDiv groups;  // eights of a row
