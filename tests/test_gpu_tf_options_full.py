@@ -42,3 +42,13 @@ def test_wide_models_match_oracle(heads, layers, seq, batch):
     _check(cfg, gpu, params, batches, "tf options, %d heads" % heads)
     _, again = _gpu_run(cfg, params, batches, "serial")
     _bits_equal(gpu, again)
+
+
+@pytest.mark.parametrize("p", [2.0 ** -18, 1.0])
+def test_extreme_dropout_matches_oracle(p):
+    """Nothing dropped (p below half a step of 2^-16), and nothing kept."""
+    cfg = synth_tf.tf_config("tf_small", **dict(ALL, dropout=p))
+    params, batches = synth_tf.make_workload(cfg, seed=22, n_batches=1)
+    print("[tf options] dropout", p, flush=True)
+    _, gpu = _gpu_run(cfg, params, batches, "serial")
+    _check(cfg, gpu, params, batches, "tf options, dropout %g" % p)
