@@ -115,8 +115,9 @@ ERASE_API erase_status erase_rope_backward(const erase_rope_config* cfg, const v
  * Layer norm over the columns of each row:
  *   m = mean(x), r = 1 / sqrt(mean((x - m)^2) + eps), h = (x - m) r, y = h w + b.
  * The variance is taken of the centred row (no difference of large sums), and
- * what the mean's own rounding leaves there is taken off the row and the variance:
- * a row of one value, however large, gives h = 0 (eps > 0). */
+ * what the mean's own rounding leaves there is taken off the row and the variance,
+ * so that rows of one value centre to zero.  (Sums are fp32: a row whose sum passes
+ * 3.4e38 has no finite mean.) */
 typedef struct {
   int64_t rows;   /* 0..2^31-1 */
   int32_t cols;   /* 1..16384 */

@@ -34,9 +34,10 @@
  *   a1 = a0 + drop(o Wo^T);  n2 = ln(a1; g2, b2);  z = a1 + drop(gelu(n2 W1^T) W2^T)
  *   l_b from ln(z; g3, b3)
  * with the operators of erase_ops.h.  With dropout a branch (o Wo^T, gelu(n2 W1^T)
- * W2^T) and the gradient at it are stored in bf16 before the mask and the sum with
- * the residual, which is rounded to bf16 again; without, the sum is formed in fp32
- * in the product's epilogue and rounded once.
+ * W2^T) is stored in bf16, then masked and added to the residual, which rounds to
+ * bf16 again; the gradient at it is the stored bf16 gradient at the sum, masked and
+ * rounded again.  Without dropout the sum is formed in fp32 in the product's
+ * epilogue and rounded once.
  */
 #ifndef ERASE_TF_H_
 #define ERASE_TF_H_
